@@ -51,7 +51,9 @@ typedef enum stalloc_status {
     STALLOC_ERR_BAD_ORDER = 6,   /* an entry of `orders` is >= n                                  */
     STALLOC_ERR_BAD_WINDOW = 7,  /* a time window with w_lo >= w_hi                               */
     STALLOC_ERR_BAD_LAYER = 8,   /* an entry of `layer_of` is >= n_layers                         */
-    STALLOC_ERR_TOO_LARGE = 9    /* the trace exceeds what an entry point without workspace holds */
+    STALLOC_ERR_TOO_LARGE = 9,   /* the trace exceeds what an entry point without workspace holds */
+    STALLOC_ERR_BAD_BOUNDS = 10, /* sequence boundaries that do not begin at 0, descend or pass the tokens */
+    STALLOC_ERR_BAD_TOKEN = 11   /* a token number beyond the vocabulary                          */
 } stalloc_status;
 
 /* Structure-of-arrays trace (Sec. 4: s, t_s, t_e of every request event). */
@@ -387,6 +389,148 @@ typedef enum stalloc_probe_kind {
 
 int stalloc_probe(uint32_t what, void *buffer, size_t buffer_bytes, uint32_t iters, uint64_t *work_done,
                   void *hip_stream);
+
+/*
+ * Operators of a training step.  A plan says where the buffers of a step lie; these operators read and
+ * write where the caller says and allocate nothing, so that a step can run at the addresses of its plan
+ * and its trace holds every byte: outputs belong to the caller, and what a call needs besides is its
+ * workspace, whose size the query gives.  Neither the scores of attention nor the probabilities of the
+ * vocabulary, the largest buffers of a step, ever exist.  Conventions as above; numbers of `dtype` in
+ * memory, sums and statistics in 32 bits or more; the results of a call do not depend on how its
+ * workgroups are scheduled.
+ */
+typedef enum stalloc_dtype {
+    STALLOC_F32 = 0,
+    STALLOC_BF16 = 1,
+    STALLOC_F16 = 2
+} stalloc_dtype;
+
+/* A tensor [tokens][heads][head_dim] on the device; strides in numbers, the last one is 1.  data must be
+ * 16-byte aligned and both strides multiples of 8 (views into a fused projection are fine). */
+typedef struct stalloc_heads {
+    void *data;
+    uint64_t token_stride;
+    uint64_t head_stride;
+} stalloc_heads;
+
+typedef struct stalloc_attention_shape {
+    uint32_t dtype;      /* STALLOC_BF16 or STALLOC_F16                                      */
+    uint32_t tokens;     /* rows of the packed batch, >= 1, < 2^31                           */
+    uint32_t sequences;  /* >= 1                                                             */
+    uint32_t heads;      /* a multiple of kv_heads; head h reads key head h * kv_heads / heads */
+    uint32_t kv_heads;
+    uint32_t head_dim;   /* a multiple of 8, at most 128                                     */
+    float scale;         /* of the scores, > 0                                               */
+} stalloc_attention_shape;
+
+/*
+ * Causal attention over packed sequences: token i of sequence [bounds[s], bounds[s+1]) sees the tokens of
+ * its sequence up to itself,
+ *     lse[h][i] = log sum_j exp(scale * q[i][h] . k[j][g]),
+ *     o[i][h] = sum_j exp(scale * q[i][h] . k[j][g] - lse[h][i]) v[j][g].
+ *
+ *   bounds        device [sequences + 1], ascending from 0 to at most `tokens`; sequences may be empty.
+ *                 Tokens behind the last boundary (padding) see nothing: o = 0, lse = -infinity.  Bounds
+ *                 that do not begin at 0, descend or pass `tokens` set device_status to
+ *                 STALLOC_ERR_BAD_BOUNDS (outputs unspecified, memory-safe).
+ *   lse           device [heads][tokens]
+ *   device_status device [1], written
+ */
+int stalloc_attention(const stalloc_attention_shape *shape, const stalloc_heads *q, const stalloc_heads *k,
+                      const stalloc_heads *v, const uint32_t *bounds, const stalloc_heads *o, float *lse,
+                      uint32_t *device_status, void *workspace, size_t *workspace_bytes, void *hip_stream);
+
+/*
+ * Gradients of the above for a gradient d_o of its output: dq, dk, dv (those of key heads summed over the
+ * heads that read them).  o and lse as written by the forward call.  Weights are computed again from q, k
+ * and lse; gradients of padding are 0.
+ */
+int stalloc_attention_backward(const stalloc_attention_shape *shape, const stalloc_heads *d_o, const stalloc_heads *q,
+                               const stalloc_heads *k, const stalloc_heads *v, const stalloc_heads *o, const float *lse,
+                               const uint32_t *bounds, const stalloc_heads *dq, const stalloc_heads *dk,
+                               const stalloc_heads *dv, uint32_t *device_status, void *workspace,
+                               size_t *workspace_bytes, void *hip_stream);
+
+/*
+ * Root-mean-square norm of every row, behind the addition of the residual:
+ *     sum = x + residual (rounded to dtype: it is what the next layer adds to),
+ *     rstd = 1 / sqrt(mean(sum^2) + eps),   y = sum * rstd * weight.
+ *
+ *   x, residual  device [rows][width], rows x_stride / residual_stride numbers apart; residual may be NULL
+ *                (sum = x then, and `sum` may be NULL as well)
+ *   sum          device [rows][width]; may be x or residual (with their stride == width)
+ *   y            device [rows][width], or NULL when only the output in 8 bits is wanted
+ *   q, scales    device [rows][width] e4m3 numbers (finite up to 448) and [rows][(width + 127) / 128] 32-bit
+ *                scales, one for every 128 columns: q * scale is y (before y is rounded to dtype) to 3 bits behind
+ *                the leading one; scale = max(max |y|, 448 * 2^-126) / 448, and NaN where a y is not
+ *                finite.  Both or neither may be NULL.
+ *   rstd         device [rows] 32-bit
+ */
+int stalloc_rms_norm(uint32_t dtype, uint32_t rows, uint32_t width, const void *x, uint64_t x_stride, const void *residual,
+                     uint64_t residual_stride, const void *weight, float eps, void *sum, void *y, uint8_t *q, float *scales,
+                     float *rstd, void *hip_stream);
+
+/*
+ * Gradients of the above: with g = weight * d_y and c = mean(g * sum) of the row,
+ *     dx = rstd * (g - sum * rstd^2 * c) + d_sum   (of x and of the residual alike),
+ *     dweight = sum over the rows of d_y * sum * rstd.
+ * All rows contiguous but d_y's, d_y_stride numbers apart.
+ *   d_sum    device [rows][width], the gradient that reaches `sum` by other ways; may be NULL.  dx may be d_sum or d_y.
+ *   dweight  device [width] 32-bit, overwritten
+ */
+int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t width, const void *d_y, uint64_t d_y_stride,
+                              const void *sum, const void *weight, const float *rstd, const void *d_sum, void *dx,
+                              float *dweight, void *workspace, size_t *workspace_bytes, void *hip_stream);
+
+/*
+ * Log probabilities of given tokens under the softmax of every row of logits, its entropy and its most
+ * likely tokens, in one pass over the logits.
+ *
+ *   logits        device [rows][vocabulary], rows row_stride numbers apart; -infinity marks a token that cannot
+ *                 occur.  A row of nothing else has lse = logprob = -infinity and entropy 0.
+ *   tokens        device [rows] int32; a negative one stands for none (logprob 0); one >= vocabulary sets
+ *                 device_status to STALLOC_ERR_BAD_TOKEN
+ *   top           how many of the most likely tokens are wanted, 0 .. min(64, vocabulary); top_tokens device
+ *                 [rows][top] int32 in descending order of their logits (lower number first among equals),
+ *                 top_logprobs device [rows][top].  (Where logits are NaN their order is unspecified.)
+ *   logprob, entropy, lse  device [rows] 32-bit, natural logarithms
+ */
+int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vocabulary, const void *logits, uint64_t row_stride,
+                           const int32_t *tokens, uint32_t top, float *logprob, float *entropy, float *lse,
+                           int32_t *top_tokens, float *top_logprobs, uint32_t *device_status, void *workspace,
+                           size_t *workspace_bytes, void *hip_stream);
+
+/*
+ * Gradient of the above with respect to the logits for gradients d_logprob and (may be NULL) d_entropy of its
+ * outputs, both device [rows]:  d_logits[j] = d_logprob * ([j = token] - p_j) - d_entropy * p_j * (log p_j + entropy).
+ * d_logits may be `logits` itself (same stride): a step then needs one such buffer.  Rows without a token take no
+ * part of d_logprob.
+ */
+int stalloc_token_logprobs_backward(uint32_t dtype, uint32_t rows, uint32_t vocabulary, const void *logits,
+                                    uint64_t row_stride, const int32_t *tokens, const float *lse, const float *entropy,
+                                    const float *d_logprob, const float *d_entropy, void *d_logits,
+                                    uint64_t d_row_stride, uint32_t *device_status, void *hip_stream);
+
+/* A tensor of a list: `count` contiguous numbers (aligned to their size), and where its clipped values go (NULL: nowhere). */
+typedef struct stalloc_tensor {
+    const void *data;
+    void *out;
+    uint64_t count;
+    uint64_t dtype;
+} stalloc_tensor;
+
+/*
+ * Norm over all tensors of a list together, and clipping to it:
+ *     norm = sqrt(sum of squares) (summed in 64 bits),   factor = min(1, max_norm / norm),   out = data * factor.
+ * A norm that is not finite leaves the numbers as they are (factor 1), so that the caller can see it and skip the
+ * step.  Where out is data and the factor is 1, nothing is written.
+ *
+ *   tensors   HOST memory, k entries; needed during the call only
+ *   max_norm  >= 0; infinity: out = data
+ *   norm, factor  device [1]
+ */
+int stalloc_clip_gradients(const stalloc_tensor *tensors, uint32_t k, float max_norm, float *norm, float *factor,
+                           void *workspace, size_t *workspace_bytes, void *hip_stream);
 
 /* Human-readable name of a stalloc_status; never NULL.  Host memory, static storage. */
 const char *stalloc_status_string(int status);

@@ -1,0 +1,204 @@
+// What the attention kernels share: matrix products of 32 x 32 tiles, tiles in LDS, and which rows of which sequence a workgroup takes.
+//
+// v_mfma_f32_32x32x16 multiplies A (32 rows x 16) by B (16 x 32 columns).  Lane l holds of A the row l % 32 and of B the
+// column l % 32, both at the positions 8 (l / 32) .. + 7 of the 16; of the result it holds the column l % 32 and the rows
+// 8 (i / 4) + 4 (l / 32) + i % 4, i = 0 .. 15.  A result with keys as rows is therefore, registers 0 .. 7 and 8 .. 15
+// taken as they are, the B operand of a product over these keys, if the other operand takes the keys in the same order:
+// positions 0 .. 3 and 4 .. 7 of half h = l / 32 stand for keys 4 h + 0 .. 3 and 8 + 4 h + 0 .. 3.  So weights never leave the
+// registers of the lane that made them.
+#pragma once
+
+#include "numbers.h"
+
+namespace stalloc {
+
+template <typename T> using V4 = typename Vec<T>::x4;
+template <typename T> using V8 = typename Vec<T>::x8;
+
+__device__ __forceinline__ f32x16 mma(V8<bf16> a, V8<bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(V8<f16> a, V8<f16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Registers 8 s .. 8 s + 7 of a result, rounded to T, as the operand of the next product.
+template <typename T, int s> __device__ __forceinline__ V8<T> operand(const f32x16& x)
+{
+    const f32x8 v = {x[8 * s], x[8 * s + 1], x[8 * s + 2], x[8 * s + 3], x[8 * s + 4], x[8 * s + 5], x[8 * s + 6], x[8 * s + 7]};
+    return __builtin_convertvector(v, V8<T>);
+}
+
+// The row (of the result tile) that register i of a lane holds.
+__device__ __forceinline__ uint32_t row_of(int i, uint32_t half) { return 8 * (i / 4) + 4 * half + i % 4; }
+
+// The same lane of the other half of the wave.
+__device__ __forceinline__ float across(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(as_bits(v), as_bits(v), false, false);
+    return as_float(lane_id() < 32 ? r[1] : r[0]);
+}
+
+// A tile of rows of kD numbers in LDS.  16-byte pieces of a row change places with the row's number, so that the lanes of one access,
+// which are in different rows at the same column, reach all banks:
+//   kAlong  for reads of 16 bytes along a row (one row per lane)
+//   kCross  for transposing reads, in which 16 lanes take 32 bytes of each of four rows
+// Where a tile is read both ways the second one serves (pairs of pieces stay together).
+enum class Order { kAlong, kCross };
+template <int kD, Order kOrder> __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece)
+{
+    constexpr uint32_t kPieces = kD / 8;
+    const uint32_t turn = kOrder == Order::kAlong ? row & (kPieces - 1) : (row << 1) & (kPieces - 1);
+    return row * kD + ((piece ^ turn) << 3);
+}
+
+template <typename T, int kD, Order kOrder> __device__ __forceinline__ V8<T> read_along(const T* tile, uint32_t row, uint32_t piece)
+{
+    return *(const V8<T>*)(tile + place<kD, kOrder>(row, piece));
+}
+
+// The A operand of a product over 16 rows of the tile (from row `base`, a multiple of 16) for 32 of its columns from column `col`: lane l gets
+// column col + l % 32 and the rows in the order of `operand`.  A transposing read gives lane i of 16 the i-th column of
+// four rows, whose quarters its neighbours point at.
+template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const T* tile, uint32_t base, uint32_t col)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const uint32_t l = lane_id(), i = l & 15, c = col + 16 * ((l >> 4) & 1) + 4 * (i & 3), row = base + 4 * (l >> 5) + (i >> 2);
+    const T* at = tile + place<kD, Order::kCross>(row, c >> 3) + (c & 7);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * kD));     // (the row eight further on turns the same way)
+    const V4<T> a = __builtin_bit_cast(V4<T>, lo), b = __builtin_bit_cast(V4<T>, hi);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// kRows rows of a tensor on their way to LDS: 16 bytes per thread and step, held in registers between `fetch` and `put`.  Rows from `last`
+// on repeat row `last`, columns from head_dim on are zeros.
+template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Staged {
+    static constexpr int kPieces = kD / 8, kSteps = kRows * kPieces / kThreads;
+    static_assert(kSteps * kThreads == kRows * kPieces, "whole steps");
+    V8<T> v[kSteps];
+
+    __device__ __forceinline__ void fetch(const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
+    {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const uint32_t at = s * kThreads + threadIdx.x, piece = at % kPieces, row = umin(first + at / kPieces, last);
+            if (kFull || piece * 8 < head_dim) v[s] = *(const V8<T>*)(data + row * stride + piece * 8);
+            else v[s] = V8<T>{};
+        }
+    }
+    template <Order kOrder> __device__ __forceinline__ void put(T* tile) const
+    {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const uint32_t at = s * kThreads + threadIdx.x;
+            *(V8<T>*)(tile + place<kD, kOrder>(at / kPieces, at % kPieces)) = v[s];
+        }
+    }
+};
+
+// One row per lane (row l % 32 of a tile) as the operand of products over the columns: step c holds columns 16 c + 8 (l / 32) .. + 7.
+template <typename T, int kD, bool kFull> __device__ __forceinline__ void load_row(V8<T> (&v)[kD / 16], const T* row, uint32_t head_dim)
+{
+    const uint32_t half = lane_id() >> 5;
+#pragma unroll
+    for (int c = 0; c < kD / 16; ++c) {
+        const uint32_t col = 16 * c + 8 * half;
+        if (kFull || col < head_dim) v[c] = *(const V8<T>*)(row + col);
+        else v[c] = V8<T>{};
+    }
+}
+
+// A result tile [columns of a head, in tiles of 32][rows] to memory: the lane's row, four neighbouring columns at a time.
+template <typename T, int kD, bool kFull> __device__ __forceinline__ void store_row(T* row, const f32x16 (&x)[kD / 32], float factor, uint32_t head_dim)
+{
+    const uint32_t half = lane_id() >> 5;
+#pragma unroll
+    for (int d = 0; d < kD / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t col = 32 * d + 8 * i + 4 * half;
+            typedef float f32x4 __attribute__((ext_vector_type(4)));
+            const f32x4 v = {x[d][4 * i] * factor, x[d][4 * i + 1] * factor, x[d][4 * i + 2] * factor, x[d][4 * i + 3] * factor};
+            if (kFull || col < head_dim) *(V4<T>*)(row + col) = __builtin_convertvector(v, V4<T>);
+        }
+}
+
+// Tensor of a call: numbers, and strides between tokens and heads.
+template <typename T> struct Heads {
+    T* data;
+    uint64_t token, head;
+    __device__ __forceinline__ T* at(uint64_t t, uint32_t h) const { return data + t * token + h * head; }
+};
+
+// kRows rows of one sequence, or of the padding behind the last one (no_keys).
+struct Piece {
+    uint32_t begin, end;                                     // the sequence
+    uint32_t first;                                          // first row of the piece; first >= end: nothing to do
+    bool no_keys;
+};
+
+// The `index`-th piece of the packed batch, every sequence cut into pieces of kRows rows from its beginning.  Sequences are counted through 64
+// at a time; boundaries are held to the batch, whatever they say, so that nothing is read or written outside of it.
+template <int kRows> __device__ __forceinline__ Piece find_piece(const uint32_t* __restrict__ bounds, uint32_t sequences, uint32_t tokens, uint32_t index)
+{
+    uint32_t before = 0;
+    for (uint32_t s = 0; s < sequences; s += kWave) {
+        const uint32_t i = s + lane_id();
+        uint32_t lo = 0, hi = 0;
+        if (i < sequences) {
+            lo = umin(bounds[i], tokens);
+            hi = umax(lo, umin(bounds[i + 1], tokens));
+        }
+        const uint32_t n = (hi - lo + kRows - 1) / kRows, upto = wave_scan_add(n), total = read_lane(upto, kWave - 1);
+        if (index - before < total) {
+            const int at = __builtin_ctzll(__ballot(upto > index - before));
+            const uint32_t from = before + read_lane(upto, at) - read_lane(n, at);
+            const uint32_t begin = read_lane(lo, at);
+            return {begin, read_lane(hi, at), begin + (index - from) * kRows, false};
+        }
+        before += total;
+    }
+    const uint32_t end = uniform(umin(bounds[sequences], tokens));
+    const uint64_t first = end + (uint64_t)(index - before) * kRows;
+    return {end, tokens, first < tokens ? (uint32_t)first : tokens, true};
+}
+
+// How many pieces a batch can have at most.
+inline uint64_t most_pieces(uint32_t tokens, uint32_t sequences, uint32_t rows) { return (uint64_t)tokens / rows + sequences + 1; }
+
+// The workgroup's place in the work when it is spread over the 8 dies: workgroups go to them in turn, so each die takes a contiguous share,
+// and neighbours (pieces that read the same keys) share an L2.
+__device__ __forceinline__ uint32_t place_in_work(uint32_t id, uint32_t n)
+{
+    const uint32_t share = n / 8, more = n % 8, die = id % 8;
+    return die * share + umin(die, more) + id / 8;
+}
+
+// The first workgroup's look at all boundaries.
+__device__ __forceinline__ void check_bounds(const uint32_t* __restrict__ bounds, uint32_t sequences, uint32_t tokens, uint32_t* status)
+{
+    __shared__ uint32_t bad;
+    if (threadIdx.x == 0) bad = bounds[0] != 0;
+    __syncthreads();
+    bool wrong = false;
+    for (uint32_t i = threadIdx.x; i < sequences; i += blockDim.x) wrong |= bounds[i] > bounds[i + 1] || bounds[i + 1] > tokens;
+    if (wrong) bad = 1;
+    __syncthreads();
+    if (threadIdx.x == 0) *status = bad ? STALLOC_ERR_BAD_BOUNDS : STALLOC_OK;
+}
+
+inline bool shape_ok(const stalloc_attention_shape* s)
+{
+    return s && (s->dtype == STALLOC_BF16 || s->dtype == STALLOC_F16) && s->tokens >= 1 && s->tokens < 0x80000000u && s->sequences >= 1 &&
+           s->sequences < 0x80000000u && s->kv_heads >= 1 && s->heads >= s->kv_heads && s->heads % s->kv_heads == 0 && s->heads < 0x10000u &&
+           s->head_dim >= 8 && s->head_dim <= 128 && s->head_dim % 8 == 0 && s->scale > 0.f && s->scale < 1e8f;
+}
+
+inline bool heads_ok(const stalloc_heads* t, const stalloc_attention_shape* s, uint32_t heads, bool written)
+{
+    if (!t || !t->data || !aligned(t->data, 16) || t->token_stride % 8 || t->head_stride % 8) return false;
+    if (t->token_stride >> 40 || t->head_stride >> 40) return false;
+    return !written || ((s->tokens == 1 || t->token_stride >= s->head_dim) && (heads == 1 || t->head_stride >= s->head_dim));
+}
+
+template <typename T> inline Heads<T> heads_of(const stalloc_heads* t) { return {static_cast<T*>(t->data), t->token_stride, t->head_stride}; }
+
+}  // namespace stalloc

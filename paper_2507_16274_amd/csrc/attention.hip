@@ -1,0 +1,159 @@
+// stalloc_attention: causal attention over packed sequences, scores and weights in registers.
+//
+//     o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i),  lse_i = log sum_{j <= i} exp(scale q_i . k_j)
+//
+// A workgroup of four waves takes 128 rows of one head, a wave 32 of them; keys and values pass through LDS 64 at a time.  A
+// wave computes the transposed scores K Q^T (keys as rows), so that a row's scores are in two lanes only: maximum and sum are taken in
+// registers, and the weights are, where they lie, the operand of the next product V^T P^T (attention.h).
+#include "attention.h"
+
+namespace stalloc {
+
+template <typename T> struct AttentionArgs {
+    Heads<T> q, k, v, o;
+    float* lse;
+    const uint32_t* bounds;
+    uint32_t* status;
+    uint32_t tokens, sequences, heads, group, head_dim, pieces;
+    float scale;
+};
+
+constexpr int kAttnThreads = 256, kAttnRows = 128, kAttnKeys = 64;
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, 2) attention_rows(AttentionArgs<T> a)
+{
+    __shared__ T keys[2][kAttnKeys * kD], values[2][kAttnKeys * kD];
+    if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
+    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
+    const Piece p = find_piece<kAttnRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
+    if (p.first >= p.end) return;
+    const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
+    if (p.no_keys) {
+        if (row < p.end) {
+            const f32x16 zero[kD / 32] = {};
+            store_row<T, kD, kFull>(a.o.at(row, head), zero, 0.f, a.head_dim);
+            if (half == 0) a.lse[(uint64_t)head * a.tokens + row] = -INFINITY;
+        }
+        return;
+    }
+    const uint32_t last = p.end - 1, kv = head / a.group;
+    const T* k = a.k.at(0, kv);
+    const T* v = a.v.at(0, kv);
+    V8<T> q[kD / 16];
+    load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
+
+    const float scale = a.scale * kLog2e, slack = 8.f / scale;
+    float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
+    f32x16 o[kD / 32] = {};
+    const uint32_t steps = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
+    Staged<T, kD, kAttnKeys, kAttnThreads, kFull> next_k, next_v;
+    next_k.fetch(k, a.k.token, p.begin, last, a.head_dim);
+    next_v.fetch(v, a.v.token, p.begin, last, a.head_dim);
+    next_k.template put<Order::kAlong>(keys[0]);
+    next_v.template put<Order::kCross>(values[0]);
+    __syncthreads();
+    for (uint32_t step = 0; step < steps; ++step) {
+        const uint32_t key = p.begin + step * kAttnKeys;
+        const T* tile_k = keys[step & 1];
+        const T* tile_v = values[step & 1];
+        if (step + 1 < steps) {
+            next_k.fetch(k, a.k.token, key + kAttnKeys, last, a.head_dim);
+            next_v.fetch(v, a.v.token, key + kAttnKeys, last, a.head_dim);
+        }
+        if (key <= first + 31) {                             // (else none of the wave's rows sees any of these keys)
+            f32x16 s[2] = {};
+#pragma unroll
+            for (int c = 0; c < kD / 16; ++c)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    s[t] = mma(read_along<T, kD, Order::kAlong>(tile_k, 32 * t + (lane_id() & 31), 2 * c + half), q[c], s[t]);
+            if (key + kAttnKeys - 1 > first) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key + 32 * t + row_of(i, half) > row) s[t][i] = -INFINITY;
+            }
+            float most = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
+            most = fmaxf(most, across(most));
+            // The maximum is raised only where weights would pass 2^8 otherwise: sums and results are relative to it all the same.
+            if (__any(most > m + slack)) {
+                const float raised = fmaxf(m, most), f = exp2_fast((m - raised) * scale);
+                m = raised;
+                total *= f;
+#pragma unroll
+                for (int d = 0; d < kD / 32; ++d) o[d] *= f;
+            }
+            const float shift = m * scale;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[t][i] = exp2_fast(__builtin_fmaf(s[t][i], scale, -shift));
+                    total += s[t][i];
+                }
+            // Weights are rounded to T for the product (half a step of T each, and of alternating sign); their sum is not.
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const V8<T> w0 = operand<T, 0>(s[t]), w1 = operand<T, 1>(s[t]);
+#pragma unroll
+                for (int d = 0; d < kD / 32; ++d) {
+                    o[d] = mma(read_cross<T, kD>(tile_v, 32 * t, 32 * d), w0, o[d]);
+                    o[d] = mma(read_cross<T, kD>(tile_v, 32 * t + 16, 32 * d), w1, o[d]);
+                }
+            }
+        }
+        if (step + 1 < steps) {
+            next_k.template put<Order::kAlong>(keys[(step + 1) & 1]);
+            next_v.template put<Order::kCross>(values[(step + 1) & 1]);
+        }
+        __syncthreads();
+    }
+    total += across(total);
+    if (row >= p.end) return;
+    store_row<T, kD, kFull>(a.o.at(row, head), o, total == 0.f ? 0.f : 1.f / total, a.head_dim);
+    if (half == 0) a.lse[(uint64_t)head * a.tokens + row] = (m * scale + log2f(total)) * kLn2;
+}
+
+}  // namespace stalloc
+
+using namespace stalloc;
+
+namespace {
+
+template <typename T> void launch_attention(const stalloc_attention_shape* s, const AttentionArgs<T>& a, uint32_t blocks, hipStream_t stream)
+{
+    const auto one = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kAttnThreads), 0, stream, a); };
+    if (s->head_dim == 128) one(attention_rows<T, 128, true>);
+    else if (s->head_dim > 64) one(attention_rows<T, 128, false>);
+    else if (s->head_dim == 64) one(attention_rows<T, 64, true>);
+    else one(attention_rows<T, 64, false>);
+}
+
+}  // namespace
+
+extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const stalloc_heads* q, const stalloc_heads* k,
+                                 const stalloc_heads* v, const uint32_t* bounds, const stalloc_heads* o, float* lse,
+                                 uint32_t* device_status, void* workspace, size_t* workspace_bytes, void* hip_stream)
+{
+    if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
+    if (!workspace) { *workspace_bytes = kAlign; return STALLOC_OK; }    // (nothing is kept in it)
+    if (!heads_ok(q, shape, shape->heads, false) || !heads_ok(k, shape, shape->kv_heads, false) || !heads_ok(v, shape, shape->kv_heads, false) ||
+        !heads_ok(o, shape, shape->heads, true) || !bounds || !lse || !device_status)
+        return STALLOC_ERR_INVALID_ARG;
+    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAttnRows), blocks = pieces * shape->heads;
+    if (blocks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    with_type(shape->dtype, [&](auto t) {
+        using T = decltype(t);
+        if constexpr (sizeof(T) == 2) {
+            const AttentionArgs<T> a = {heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), lse, bounds, device_status, shape->tokens,
+                                        shape->sequences, shape->heads, shape->heads / shape->kv_heads, shape->head_dim, (uint32_t)pieces, shape->scale};
+            launch_attention<T>(shape, a, (uint32_t)blocks, static_cast<hipStream_t>(hip_stream));
+        }
+    });
+    return launched();
+}

@@ -1,0 +1,240 @@
+// stalloc_attention_backward: gradients of causal attention over packed sequences, weights computed again from lse.
+//
+//     p_ij = exp(scale q_i . k_j - lse_i),  D_i = do_i . o_i,  ds_ij = scale p_ij (do_i . v_j - D_i)
+//     dq_i = sum_j ds_ij k_j,   dk_j = sum_h sum_i ds_ij q_i,   dv_j = sum_h sum_i p_ij do_i
+//
+// Three kernels: D; dk and dv, a workgroup per 128 keys that goes through all rows that see them, of all heads that share them; dq, a workgroup per
+// 128 rows of a head.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave:
+// no atomics, no partial gradients in memory, and the same result every time.
+#include "attention.h"
+
+namespace stalloc {
+
+template <typename T> struct AttentionBackwardArgs {
+    Heads<T> d_o, q, k, v, o, dq, dk, dv;
+    const float* lse;
+    float* dots;                                             // [heads][tokens]: D
+    const uint32_t* bounds;
+    uint32_t* status;
+    uint32_t tokens, sequences, heads, group, head_dim, pieces;
+    float scale;
+};
+
+constexpr int kAbThreads = 256, kAbRows = 128, kAbKeys = 64, kAbStep = 32;
+
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += dpp<kDppRowRor8>(0.f, v);
+    v += dpp<kDppRowRor4>(0.f, v);
+    v += dpp<kDppRowRor2>(0.f, v);
+    v += dpp<kDppRowRor1>(0.f, v);
+    return v;
+}
+
+// D: 16 lanes take a row of one head.
+template <typename T> __global__ void __launch_bounds__(256) attention_dots(AttentionBackwardArgs<T> a)
+{
+    const uint64_t at = (uint64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (at >= (uint64_t)a.tokens * a.heads) return;
+    const uint32_t token = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads), col = (threadIdx.x & 15) * 8;
+    float v = 0.f;
+    if (col < a.head_dim) {
+        const f32x8 x = load8(a.d_o.at(token, head) + col), y = load8(a.o.at(token, head) + col);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v = __builtin_fmaf(x[i], y[i], v);
+    }
+    v = row_sum(v);
+    if (col == 0) a.dots[(uint64_t)head * a.tokens + token] = v;
+}
+
+// lse in units of log 2; a row that saw nothing weighs nothing.
+__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 1) attention_dk_dv(AttentionBackwardArgs<T> a)
+{
+    __shared__ T rows_q[2][kAbStep * kD], rows_do[2][kAbStep * kD];
+    __shared__ float row_lse[2][kAbStep], row_dot[2][kAbStep];
+    if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
+    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), kv = work / a.pieces;
+    const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, work % a.pieces);           // keys that many rows see first
+    if (p.first >= p.end) return;
+    const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), key = first + (lane_id() & 31);
+    f32x16 dk[kD / 32] = {}, dv[kD / 32] = {};
+    if (!p.no_keys) {
+        const uint32_t last = p.end - 1;
+        V8<T> k[kD / 16], v[kD / 16];
+        load_row<T, kD, kFull>(k, a.k.at(umin(key, last), kv), a.head_dim);
+        load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
+        const float scale = a.scale * kLog2e;
+        const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, steps = per_head * a.group;
+        Staged<T, kD, kAbStep, kAbThreads, kFull> next_q, next_do;
+        float next_lse = 0.f, next_dot = 0.f;
+        const auto fetch = [&](uint32_t step) {
+            const uint32_t head = kv * a.group + step / per_head, row = p.first + step % per_head * kAbStep;
+            next_q.fetch(a.q.at(0, head), a.q.token, row, last, a.head_dim);
+            next_do.fetch(a.d_o.at(0, head), a.d_o.token, row, last, a.head_dim);
+            const uint32_t mine = row + (threadIdx.x & (kAbStep - 1));
+            next_lse = mine < p.end ? lse2_of(a.lse[(uint64_t)head * a.tokens + mine]) : INFINITY;   // rows past the sequence weigh nothing
+            next_dot = a.dots[(uint64_t)head * a.tokens + umin(mine, last)];
+        };
+        const auto put = [&](uint32_t to) {
+            next_q.template put<Order::kCross>(rows_q[to]);
+            next_do.template put<Order::kCross>(rows_do[to]);
+            if (threadIdx.x < kAbStep) {
+                row_lse[to][threadIdx.x] = next_lse;
+                row_dot[to][threadIdx.x] = next_dot;
+            }
+        };
+        fetch(0);
+        put(0);
+        __syncthreads();
+        for (uint32_t step = 0; step < steps; ++step) {
+            const uint32_t now = step & 1, row = p.first + step % per_head * kAbStep;
+            if (step + 1 < steps) fetch(step + 1);
+            if (row + kAbStep - 1 >= first) {                // (else none of these rows sees a key of this wave)
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int c = 0; c < kD / 16; ++c) {
+                    s = mma(read_along<T, kD, Order::kCross>(rows_q[now], lane_id() & 31, 2 * c + half), k[c], s);
+                    dp = mma(read_along<T, kD, Order::kCross>(rows_do[now], lane_id() & 31, 2 * c + half), v[c], dp);
+                }
+                const bool crosses = row < first + 31;       // some of these rows do not see some of these keys
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t r = row_of(i, half);
+                    float w = exp2_fast(__builtin_fmaf(s[i], scale, -row_lse[now][r]));
+                    float d = w * (dp[i] - row_dot[now][r]) * a.scale;
+                    if (crosses && row + r < key) w = d = 0.f;
+                    s[i] = w;
+                    dp[i] = d;
+                }
+                // Weights and their gradients are rounded to T for the products; sums stay in 32 bits.
+                const V8<T> w0 = operand<T, 0>(s), w1 = operand<T, 1>(s), d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
+#pragma unroll
+                for (int d = 0; d < kD / 32; ++d) {
+                    dv[d] = mma(read_cross<T, kD>(rows_do[now], 0, 32 * d), w0, dv[d]);
+                    dv[d] = mma(read_cross<T, kD>(rows_do[now], 16, 32 * d), w1, dv[d]);
+                    dk[d] = mma(read_cross<T, kD>(rows_q[now], 0, 32 * d), d0, dk[d]);
+                    dk[d] = mma(read_cross<T, kD>(rows_q[now], 16, 32 * d), d1, dk[d]);
+                }
+            }
+            if (step + 1 < steps) put(now ^ 1);
+            __syncthreads();
+        }
+    }
+    if (key >= p.end) return;
+    store_row<T, kD, kFull>(a.dk.at(key, kv), dk, 1.f, a.head_dim);
+    store_row<T, kD, kFull>(a.dv.at(key, kv), dv, 1.f, a.head_dim);
+}
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dq(AttentionBackwardArgs<T> a)
+{
+    __shared__ T keys[2][kAbKeys * kD], values[2][kAbKeys * kD];
+    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
+    const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
+    if (p.first >= p.end) return;
+    const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
+    f32x16 dq[kD / 32] = {};
+    if (!p.no_keys) {
+        const uint32_t last = p.end - 1, kv = head / a.group, mine = umin(row, last);
+        const T* k = a.k.at(0, kv);
+        const T* v = a.v.at(0, kv);
+        V8<T> q[kD / 16], d_o[kD / 16];
+        load_row<T, kD, kFull>(q, a.q.at(mine, head), a.head_dim);
+        load_row<T, kD, kFull>(d_o, a.d_o.at(mine, head), a.head_dim);
+        const float lse = lse2_of(a.lse[(uint64_t)head * a.tokens + mine]), dots = a.dots[(uint64_t)head * a.tokens + mine], scale = a.scale * kLog2e;
+        const uint32_t steps = (umin(p.first + kAbRows, p.end) - p.begin + kAbKeys - 1) / kAbKeys;
+        Staged<T, kD, kAbKeys, kAbThreads, kFull> next_k, next_v;
+        next_k.fetch(k, a.k.token, p.begin, last, a.head_dim);
+        next_v.fetch(v, a.v.token, p.begin, last, a.head_dim);
+        next_k.template put<Order::kCross>(keys[0]);
+        next_v.template put<Order::kAlong>(values[0]);
+        __syncthreads();
+        for (uint32_t step = 0; step < steps; ++step) {
+            const uint32_t key = p.begin + step * kAbKeys;
+            const T* tile_k = keys[step & 1];
+            const T* tile_v = values[step & 1];
+            if (step + 1 < steps) {
+                next_k.fetch(k, a.k.token, key + kAbKeys, last, a.head_dim);
+                next_v.fetch(v, a.v.token, key + kAbKeys, last, a.head_dim);
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (key + 32 * t > first + 31) break;        // (none of the wave's rows sees any of these keys)
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int c = 0; c < kD / 16; ++c) {
+                    s = mma(read_along<T, kD, Order::kCross>(tile_k, 32 * t + (lane_id() & 31), 2 * c + half), q[c], s);
+                    dp = mma(read_along<T, kD, Order::kAlong>(tile_v, 32 * t + (lane_id() & 31), 2 * c + half), d_o[c], dp);
+                }
+                const bool crosses = key + 32 * t + 31 > first;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = exp2_fast(__builtin_fmaf(s[i], scale, -lse));
+                    dp[i] = w * (dp[i] - dots) * a.scale;
+                    if (crosses && key + 32 * t + row_of(i, half) > row) dp[i] = 0.f;
+                }
+                const V8<T> d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
+#pragma unroll
+                for (int d = 0; d < kD / 32; ++d) {
+                    dq[d] = mma(read_cross<T, kD>(tile_k, 32 * t, 32 * d), d0, dq[d]);
+                    dq[d] = mma(read_cross<T, kD>(tile_k, 32 * t + 16, 32 * d), d1, dq[d]);
+                }
+            }
+            if (step + 1 < steps) {
+                next_k.template put<Order::kCross>(keys[(step + 1) & 1]);
+                next_v.template put<Order::kAlong>(values[(step + 1) & 1]);
+            }
+            __syncthreads();
+        }
+    }
+    if (row < p.end) store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
+}
+
+}  // namespace stalloc
+
+using namespace stalloc;
+
+namespace {
+
+template <typename T, int kD, bool kFull> void launch_backward(const AttentionBackwardArgs<T>& a, hipStream_t stream)
+{
+    hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.pieces * (a.heads / a.group)), dim3(kAbThreads), 0, stream, a);
+    hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.pieces * a.heads), dim3(kAbThreads), 0, stream, a);
+}
+
+}  // namespace
+
+extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, const stalloc_heads* d_o, const stalloc_heads* q,
+                                          const stalloc_heads* k, const stalloc_heads* v, const stalloc_heads* o, const float* lse,
+                                          const uint32_t* bounds, const stalloc_heads* dq, const stalloc_heads* dk,
+                                          const stalloc_heads* dv, uint32_t* device_status, void* workspace,
+                                          size_t* workspace_bytes, void* hip_stream)
+{
+    if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
+    const uint32_t heads = shape->heads, kv = shape->kv_heads;
+    Carver cv(workspace);
+    float* dots = cv.take<float>((size_t)shape->tokens * heads);
+    if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
+    if (!heads_ok(d_o, shape, heads, false) || !heads_ok(q, shape, heads, false) || !heads_ok(k, shape, kv, false) || !heads_ok(v, shape, kv, false) ||
+        !heads_ok(o, shape, heads, false) || !heads_ok(dq, shape, heads, true) || !heads_ok(dk, shape, kv, true) || !heads_ok(dv, shape, kv, true) ||
+        !lse || !bounds || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
+        return STALLOC_ERR_INVALID_ARG;
+    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows), rows = ((uint64_t)shape->tokens * heads + 15) / 16;
+    if (pieces * heads > 0x7fffffffu || rows > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    with_type(shape->dtype, [&](auto t) {
+        using T = decltype(t);
+        if constexpr (sizeof(T) == 2) {
+            const AttentionBackwardArgs<T> a = {heads_of<T>(d_o), heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), heads_of<T>(dq),
+                                                heads_of<T>(dk), heads_of<T>(dv), lse, dots, bounds, device_status, shape->tokens, shape->sequences,
+                                                heads, heads / kv, shape->head_dim, (uint32_t)pieces, shape->scale};
+            hipLaunchKernelGGL(attention_dots<T>, dim3((uint32_t)rows), dim3(256), 0, stream, a);
+            if (shape->head_dim == 128) launch_backward<T, 128, true>(a, stream);
+            else if (shape->head_dim > 64) launch_backward<T, 128, false>(a, stream);
+            else if (shape->head_dim == 64) launch_backward<T, 64, true>(a, stream);
+            else launch_backward<T, 64, false>(a, stream);
+        }
+    });
+    return launched();
+}

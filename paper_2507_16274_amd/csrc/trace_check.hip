@@ -101,6 +101,8 @@ extern "C" const char* stalloc_status_string(int status)
         case STALLOC_ERR_BAD_WINDOW: return "STALLOC_ERR_BAD_WINDOW";
         case STALLOC_ERR_BAD_LAYER: return "STALLOC_ERR_BAD_LAYER";
         case STALLOC_ERR_TOO_LARGE: return "STALLOC_ERR_TOO_LARGE";
+        case STALLOC_ERR_BAD_BOUNDS: return "STALLOC_ERR_BAD_BOUNDS";
+        case STALLOC_ERR_BAD_TOKEN: return "STALLOC_ERR_BAD_TOKEN";
         default: return "STALLOC_UNKNOWN_STATUS";
     }
 }

@@ -68,31 +68,43 @@ template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const 
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// kRows rows of a tensor on their way to LDS: 16 bytes per thread and step, held in registers between `fetch` and `put`.  Rows from `last`
-// on repeat row `last`, columns from head_dim on are zeros.
-template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Staged {
-    static constexpr int kPieces = kD / 8, kSteps = kRows * kPieces / kThreads;
-    static_assert(kSteps * kThreads == kRows * kPieces, "whole steps");
-    V8<T> v[kSteps];
+// kRows rows of a tensor on their way to LDS, 16 bytes per lane and access, without a register between: the memory pipe writes 64 lanes' pieces one
+// behind the other, so a lane asks for the piece that belongs where its own lands.  Rows past `last` repeat it; columns from head_dim
+// on are left as they are (the kernel has cleared them).  `first` <= `last`; kLoads accesses of every wave, counted by vmcnt.
+template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Rows {
+    static constexpr int kPieces = kD / 8, kLoads = kRows * kPieces / kThreads;
+    static_assert(kLoads * kThreads == kRows * kPieces, "whole accesses");
 
-    __device__ __forceinline__ void fetch(const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
+    template <Order kOrder> static __device__ __forceinline__ void fetch(T* tile, const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
     {
+        typedef __attribute__((address_space(3))) void* lds_ptr;
+        typedef const __attribute__((address_space(1))) void* global_ptr;
+        const char* base = (const char*)(data + first * stride);
+        const uint32_t bytes = (uint32_t)stride * sizeof(T), most = last - first;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const uint32_t at = s * kThreads + threadIdx.x, piece = at % kPieces, row = umin(first + at / kPieces, last);
-            if (kFull || piece * 8 < head_dim) v[s] = *(const V8<T>*)(data + row * stride + piece * 8);
-            else v[s] = V8<T>{};
-        }
-    }
-    template <Order kOrder> __device__ __forceinline__ void put(T* tile) const
-    {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const uint32_t at = s * kThreads + threadIdx.x;
-            *(V8<T>*)(tile + place<kD, kOrder>(at / kPieces, at % kPieces)) = v[s];
+        for (int s = 0; s < kLoads; ++s) {
+            const uint32_t at = s * kThreads + threadIdx.x, row = at / kPieces, piece = (at % kPieces) ^ (place<kD, kOrder>(row, 0) / 8 % kPieces);
+            const uint32_t offset = umin(row, most) * bytes + piece * 16;
+            if (kFull || piece * 8 < head_dim)
+                __builtin_amdgcn_global_load_lds((global_ptr)(base + offset), (lds_ptr)(tile + (s * kThreads + wave_id() * kWave) * 8), 16, 0, 0);
         }
     }
 };
+
+// The tiles that the wave's accesses were asked for before the last `kLater` ones have landed, its own reads are done, and so are the other
+// waves': behind this the tile may be read, and the one read before it written.
+template <int kLater> __device__ __forceinline__ void tiles_landed()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLater) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int kWords, int kThreads> __device__ __forceinline__ void clear_lds(void* lds)
+{
+    for (int i = threadIdx.x; i < kWords / 4; i += kThreads) ((uint4*)lds)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+}
 
 // One row per lane (row l % 32 of a tile) as the operand of products over the columns: step c holds columns 16 c + 8 (l / 32) .. + 7.
 template <typename T, int kD, bool kFull> __device__ __forceinline__ void load_row(V8<T> (&v)[kD / 16], const T* row, uint32_t head_dim)
@@ -185,6 +197,8 @@ __device__ __forceinline__ void check_bounds(const uint32_t* __restrict__ bounds
     if (threadIdx.x == 0) *status = bad ? STALLOC_ERR_BAD_BOUNDS : STALLOC_OK;
 }
 
+constexpr uint64_t kMostStride = 1u << 24;
+
 inline bool shape_ok(const stalloc_attention_shape* s)
 {
     return s && (s->dtype == STALLOC_BF16 || s->dtype == STALLOC_F16) && s->tokens >= 1 && s->tokens < 0x80000000u && s->sequences >= 1 &&
@@ -195,7 +209,7 @@ inline bool shape_ok(const stalloc_attention_shape* s)
 inline bool heads_ok(const stalloc_heads* t, const stalloc_attention_shape* s, uint32_t heads, bool written)
 {
     if (!t || !t->data || !aligned(t->data, 16) || t->token_stride % 8 || t->head_stride % 8) return false;
-    if (t->token_stride >> 40 || t->head_stride >> 40) return false;
+    if (t->token_stride > kMostStride || t->head_stride >> 40) return false;     // (offsets inside a tile have 32 bits)
     return !written || ((s->tokens == 1 || t->token_stride >= s->head_dim) && (heads == 1 || t->head_stride >= s->head_dim));
 }
 

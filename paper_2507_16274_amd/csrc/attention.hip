@@ -18,11 +18,11 @@ template <typename T> struct AttentionArgs {
     float scale;
 };
 
-constexpr int kAttnThreads = 256, kAttnRows = 128, kAttnKeys = 64;
+constexpr int kAttnThreads = 256, kAttnRows = 128, kAttnKeys = 64, kAttnStages = 2;
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, 2) attention_rows(AttentionArgs<T> a)
 {
-    __shared__ T keys[2][kAttnKeys * kD], values[2][kAttnKeys * kD];
+    __shared__ T ring[kAttnStages][2][kAttnKeys * kD];       // keys, values
     if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
     const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
     const Piece p = find_piece<kAttnRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
@@ -46,19 +46,25 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
     f32x16 o[kD / 32] = {};
     const uint32_t steps = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
-    Staged<T, kD, kAttnKeys, kAttnThreads, kFull> next_k, next_v;
-    next_k.fetch(k, a.k.token, p.begin, last, a.head_dim);
-    next_v.fetch(v, a.v.token, p.begin, last, a.head_dim);
-    next_k.template put<Order::kAlong>(keys[0]);
-    next_v.template put<Order::kCross>(values[0]);
-    __syncthreads();
+    using Tile = Rows<T, kD, kAttnKeys, kAttnThreads, kFull>;
+    const auto fetch = [&](uint32_t step) {
+        T (&stage)[2][kAttnKeys * kD] = ring[step % kAttnStages];
+        Tile::template fetch<Order::kAlong>(stage[0], k, a.k.token, p.begin + step * kAttnKeys, last, a.head_dim);
+        Tile::template fetch<Order::kCross>(stage[1], v, a.v.token, p.begin + step * kAttnKeys, last, a.head_dim);
+    };
+    if (!kFull) clear_lds<sizeof(ring) / 4, kAttnThreads>(ring);
+#pragma unroll
+    for (uint32_t step = 0; step < kAttnStages - 1; ++step)
+        if (step < steps) fetch(step);
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t key = p.begin + step * kAttnKeys;
-        const T* tile_k = keys[step & 1];
-        const T* tile_v = values[step & 1];
-        if (step + 1 < steps) {
-            next_k.fetch(k, a.k.token, key + kAttnKeys, last, a.head_dim);
-            next_v.fetch(v, a.v.token, key + kAttnKeys, last, a.head_dim);
+        const T* tile_k = ring[step % kAttnStages][0];
+        const T* tile_v = ring[step % kAttnStages][1];
+        if (step + kAttnStages - 1 < steps) {
+            tiles_landed<2 * Tile::kLoads * (kAttnStages - 2)>();
+            fetch(step + kAttnStages - 1);
+        } else {
+            tiles_landed<0>();
         }
         if (key <= first + 31) {                             // (else none of the wave's rows sees any of these keys)
             f32x16 s[2] = {};
@@ -107,11 +113,6 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                 }
             }
         }
-        if (step + 1 < steps) {
-            next_k.template put<Order::kAlong>(keys[(step + 1) & 1]);
-            next_v.template put<Order::kCross>(values[(step + 1) & 1]);
-        }
-        __syncthreads();
     }
     total += across(total);
     if (row >= p.end) return;

@@ -13,14 +13,14 @@ namespace stalloc {
 template <typename T> struct AttentionBackwardArgs {
     Heads<T> d_o, q, k, v, o, dq, dk, dv;
     const float* lse;
-    float* dots;                                             // [heads][tokens]: D
+    f32x2* stats;                                            // [heads][tokens]: lse in units of log 2, D
     const uint32_t* bounds;
     uint32_t* status;
     uint32_t tokens, sequences, heads, group, head_dim, pieces;
     float scale;
 };
 
-constexpr int kAbThreads = 256, kAbRows = 128, kAbKeys = 64, kAbStep = 32;
+constexpr int kAbThreads = 256, kAbRows = 128, kAbStep = 32, kAbStages = 4;
 
 __device__ __forceinline__ float row_sum(float v)
 {
@@ -30,6 +30,9 @@ __device__ __forceinline__ float row_sum(float v)
     v += dpp<kDppRowRor1>(0.f, v);
     return v;
 }
+
+// lse in units of log 2; a row that saw nothing weighs nothing.
+__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
 // D: 16 lanes take a row of one head.
 template <typename T> __global__ void __launch_bounds__(256) attention_dots(AttentionBackwardArgs<T> a)
@@ -44,16 +47,14 @@ template <typename T> __global__ void __launch_bounds__(256) attention_dots(Atte
         for (int i = 0; i < 8; ++i) v = __builtin_fmaf(x[i], y[i], v);
     }
     v = row_sum(v);
-    if (col == 0) a.dots[(uint64_t)head * a.tokens + token] = v;
+    const uint64_t to = (uint64_t)head * a.tokens + token;
+    if (col == 0) a.stats[to] = f32x2{lse2_of(a.lse[to]), v};
 }
 
-// lse in units of log 2; a row that saw nothing weighs nothing.
-__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
-
-template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 1) attention_dk_dv(AttentionBackwardArgs<T> a)
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dk_dv(AttentionBackwardArgs<T> a)
 {
-    __shared__ T rows_q[2][kAbStep * kD], rows_do[2][kAbStep * kD];
-    __shared__ float row_lse[2][kAbStep], row_dot[2][kAbStep];
+    __shared__ T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
+    __shared__ f32x2 ring_stats[kAbStages][kAbThreads / kWave][kAbStep];     // (a copy per wave)
     if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
     const uint32_t work = place_in_work(blockIdx.x, gridDim.x), kv = work / a.pieces;
     const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, work % a.pieces);           // keys that many rows see first
@@ -66,60 +67,67 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         load_row<T, kD, kFull>(k, a.k.at(umin(key, last), kv), a.head_dim);
         load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
         const float scale = a.scale * kLog2e;
+        using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, steps = per_head * a.group;
-        Staged<T, kD, kAbStep, kAbThreads, kFull> next_q, next_do;
-        float next_lse = 0.f, next_dot = 0.f;
-        const auto fetch = [&](uint32_t step) {
-            const uint32_t head = kv * a.group + step / per_head, row = p.first + step % per_head * kAbStep;
-            next_q.fetch(a.q.at(0, head), a.q.token, row, last, a.head_dim);
-            next_do.fetch(a.d_o.at(0, head), a.d_o.token, row, last, a.head_dim);
-            const uint32_t mine = row + (threadIdx.x & (kAbStep - 1));
-            next_lse = mine < p.end ? lse2_of(a.lse[(uint64_t)head * a.tokens + mine]) : INFINITY;   // rows past the sequence weigh nothing
-            next_dot = a.dots[(uint64_t)head * a.tokens + umin(mine, last)];
+        uint32_t next_head = kv * a.group, next_row = p.first, next_slot = 0;
+        const auto fetch = [&]() {
+            typedef __attribute__((address_space(3))) void* lds_ptr;
+            typedef const __attribute__((address_space(1))) void* global_ptr;
+            Tile::template fetch<Order::kCross>(ring[next_slot][0], a.q.at(0, next_head), a.q.token, next_row, last, a.head_dim);
+            Tile::template fetch<Order::kCross>(ring[next_slot][1], a.d_o.at(0, next_head), a.d_o.token, next_row, last, a.head_dim);
+            const float* from = (const float*)(a.stats + (uint64_t)next_head * a.tokens + next_row);   // (room for a whole step is behind the last row)
+            __builtin_amdgcn_global_load_lds((global_ptr)(from + lane_id()), (lds_ptr)ring_stats[next_slot][wave_id()], 4, 0, 0);
+            next_row += kAbStep;
+            if (next_row >= p.end) { next_row = p.first; ++next_head; }
+            next_slot = (next_slot + 1) % kAbStages;
         };
-        const auto put = [&](uint32_t to) {
-            next_q.template put<Order::kCross>(rows_q[to]);
-            next_do.template put<Order::kCross>(rows_do[to]);
-            if (threadIdx.x < kAbStep) {
-                row_lse[to][threadIdx.x] = next_lse;
-                row_dot[to][threadIdx.x] = next_dot;
-            }
-        };
-        fetch(0);
-        put(0);
-        __syncthreads();
+        constexpr int kLoads = 2 * Tile::kLoads + 1;
+        if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
+        for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch();
+        uint32_t row = p.first, now = 0;
         for (uint32_t step = 0; step < steps; ++step) {
-            const uint32_t now = step & 1, row = p.first + step % per_head * kAbStep;
-            if (step + 1 < steps) fetch(step + 1);
+            if (step + kAbStages - 1 < steps) {
+                tiles_landed<kLoads * (kAbStages - 2)>();
+                fetch();
+            } else {
+                tiles_landed<0>();
+            }
+            const T* tile_q = ring[now][0];
+            const T* tile_do = ring[now][1];
+            const f32x2* stats = ring_stats[now][wave_id()];
             if (row + kAbStep - 1 >= first) {                // (else none of these rows sees a key of this wave)
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int c = 0; c < kD / 16; ++c) {
-                    s = mma(read_along<T, kD, Order::kCross>(rows_q[now], lane_id() & 31, 2 * c + half), k[c], s);
-                    dp = mma(read_along<T, kD, Order::kCross>(rows_do[now], lane_id() & 31, 2 * c + half), v[c], dp);
+                    s = mma(read_along<T, kD, Order::kCross>(tile_q, lane_id() & 31, 2 * c + half), k[c], s);
+                    dp = mma(read_along<T, kD, Order::kCross>(tile_do, lane_id() & 31, 2 * c + half), v[c], dp);
                 }
-                const bool crosses = row < first + 31;       // some of these rows do not see some of these keys
+                const bool crosses = row < first + 31 || row + kAbStep > p.end;      // some of these rows do not see some of these keys, or are not the sequence's
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t r = row_of(i, half);
-                    float w = exp2_fast(__builtin_fmaf(s[i], scale, -row_lse[now][r]));
-                    float d = w * (dp[i] - row_dot[now][r]) * a.scale;
-                    if (crosses && row + r < key) w = d = 0.f;
-                    s[i] = w;
-                    dp[i] = d;
+                    const f32x2 st = stats[row_of(i, half)];
+                    s[i] = exp2_fast(__builtin_fmaf(s[i], scale, -st[0]));
+                    dp[i] = s[i] * (dp[i] - st[1]) * a.scale;
                 }
+                if (crosses)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t r = row + row_of(i, half);
+                        if (r < key || r >= p.end) s[i] = dp[i] = 0.f;
+                    }
                 // Weights and their gradients are rounded to T for the products; sums stay in 32 bits.
                 const V8<T> w0 = operand<T, 0>(s), w1 = operand<T, 1>(s), d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
 #pragma unroll
                 for (int d = 0; d < kD / 32; ++d) {
-                    dv[d] = mma(read_cross<T, kD>(rows_do[now], 0, 32 * d), w0, dv[d]);
-                    dv[d] = mma(read_cross<T, kD>(rows_do[now], 16, 32 * d), w1, dv[d]);
-                    dk[d] = mma(read_cross<T, kD>(rows_q[now], 0, 32 * d), d0, dk[d]);
-                    dk[d] = mma(read_cross<T, kD>(rows_q[now], 16, 32 * d), d1, dk[d]);
+                    dv[d] = mma(read_cross<T, kD>(tile_do, 0, 32 * d), w0, dv[d]);
+                    dv[d] = mma(read_cross<T, kD>(tile_do, 16, 32 * d), w1, dv[d]);
+                    dk[d] = mma(read_cross<T, kD>(tile_q, 0, 32 * d), d0, dk[d]);
+                    dk[d] = mma(read_cross<T, kD>(tile_q, 16, 32 * d), d1, dk[d]);
                 }
             }
-            if (step + 1 < steps) put(now ^ 1);
-            __syncthreads();
+            row += kAbStep;
+            if (row >= p.end) row = p.first;
+            now = (now + 1) % kAbStages;
         }
     }
     if (key >= p.end) return;
@@ -129,7 +137,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dq(AttentionBackwardArgs<T> a)
 {
-    __shared__ T keys[2][kAbKeys * kD], values[2][kAbKeys * kD];
+    __shared__ T ring[kAbStages][2][kAbStep * kD];           // keys, values
     const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
     const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
     if (p.first >= p.end) return;
@@ -142,50 +150,50 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         V8<T> q[kD / 16], d_o[kD / 16];
         load_row<T, kD, kFull>(q, a.q.at(mine, head), a.head_dim);
         load_row<T, kD, kFull>(d_o, a.d_o.at(mine, head), a.head_dim);
-        const float lse = lse2_of(a.lse[(uint64_t)head * a.tokens + mine]), dots = a.dots[(uint64_t)head * a.tokens + mine], scale = a.scale * kLog2e;
-        const uint32_t steps = (umin(p.first + kAbRows, p.end) - p.begin + kAbKeys - 1) / kAbKeys;
-        Staged<T, kD, kAbKeys, kAbThreads, kFull> next_k, next_v;
-        next_k.fetch(k, a.k.token, p.begin, last, a.head_dim);
-        next_v.fetch(v, a.v.token, p.begin, last, a.head_dim);
-        next_k.template put<Order::kCross>(keys[0]);
-        next_v.template put<Order::kAlong>(values[0]);
-        __syncthreads();
+        const f32x2 stats = a.stats[(uint64_t)head * a.tokens + mine];
+        const float scale = a.scale * kLog2e;
+        using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
+        const uint32_t steps = (umin(p.first + kAbRows, p.end) - p.begin + kAbStep - 1) / kAbStep;
+        const auto fetch = [&](uint32_t step) {
+            T (&stage)[2][kAbStep * kD] = ring[step % kAbStages];
+            Tile::template fetch<Order::kCross>(stage[0], k, a.k.token, p.begin + step * kAbStep, last, a.head_dim);
+            Tile::template fetch<Order::kAlong>(stage[1], v, a.v.token, p.begin + step * kAbStep, last, a.head_dim);
+        };
+        if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
+        for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch(step);
         for (uint32_t step = 0; step < steps; ++step) {
-            const uint32_t key = p.begin + step * kAbKeys;
-            const T* tile_k = keys[step & 1];
-            const T* tile_v = values[step & 1];
-            if (step + 1 < steps) {
-                next_k.fetch(k, a.k.token, key + kAbKeys, last, a.head_dim);
-                next_v.fetch(v, a.v.token, key + kAbKeys, last, a.head_dim);
+            const uint32_t key = p.begin + step * kAbStep;
+            if (step + kAbStages - 1 < steps) {
+                tiles_landed<2 * Tile::kLoads * (kAbStages - 2)>();
+                fetch(step + kAbStages - 1);
+            } else {
+                tiles_landed<0>();
             }
+            const T* tile_k = ring[step % kAbStages][0];
+            const T* tile_v = ring[step % kAbStages][1];
+            if (key > first + 31) continue;                  // (none of the wave's rows sees any of these keys)
+            f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (key + 32 * t > first + 31) break;        // (none of the wave's rows sees any of these keys)
-                f32x16 s = {}, dp = {};
-#pragma unroll
-                for (int c = 0; c < kD / 16; ++c) {
-                    s = mma(read_along<T, kD, Order::kCross>(tile_k, 32 * t + (lane_id() & 31), 2 * c + half), q[c], s);
-                    dp = mma(read_along<T, kD, Order::kAlong>(tile_v, 32 * t + (lane_id() & 31), 2 * c + half), d_o[c], dp);
-                }
-                const bool crosses = key + 32 * t + 31 > first;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = exp2_fast(__builtin_fmaf(s[i], scale, -lse));
-                    dp[i] = w * (dp[i] - dots) * a.scale;
-                    if (crosses && key + 32 * t + row_of(i, half) > row) dp[i] = 0.f;
-                }
-                const V8<T> d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
-#pragma unroll
-                for (int d = 0; d < kD / 32; ++d) {
-                    dq[d] = mma(read_cross<T, kD>(tile_k, 32 * t, 32 * d), d0, dq[d]);
-                    dq[d] = mma(read_cross<T, kD>(tile_k, 32 * t + 16, 32 * d), d1, dq[d]);
-                }
+            for (int c = 0; c < kD / 16; ++c) {
+                s = mma(read_along<T, kD, Order::kCross>(tile_k, lane_id() & 31, 2 * c + half), q[c], s);
+                dp = mma(read_along<T, kD, Order::kAlong>(tile_v, lane_id() & 31, 2 * c + half), d_o[c], dp);
             }
-            if (step + 1 < steps) {
-                next_k.template put<Order::kCross>(keys[(step + 1) & 1]);
-                next_v.template put<Order::kAlong>(values[(step + 1) & 1]);
+            const bool crosses = key + 31 > first;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = exp2_fast(__builtin_fmaf(s[i], scale, -stats[0]));
+                dp[i] = w * (dp[i] - stats[1]) * a.scale;
             }
-            __syncthreads();
+            if (crosses)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key + row_of(i, half) > row) dp[i] = 0.f;
+            const V8<T> d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
+#pragma unroll
+            for (int d = 0; d < kD / 32; ++d) {
+                dq[d] = mma(read_cross<T, kD>(tile_k, 0, 32 * d), d0, dq[d]);
+                dq[d] = mma(read_cross<T, kD>(tile_k, 16, 32 * d), d1, dq[d]);
+            }
         }
     }
     if (row < p.end) store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
@@ -214,7 +222,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
     const uint32_t heads = shape->heads, kv = shape->kv_heads;
     Carver cv(workspace);
-    float* dots = cv.take<float>((size_t)shape->tokens * heads);
+    f32x2* stats = cv.take<f32x2>((size_t)shape->tokens * heads + kAbStep);
     if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
     if (!heads_ok(d_o, shape, heads, false) || !heads_ok(q, shape, heads, false) || !heads_ok(k, shape, kv, false) || !heads_ok(v, shape, kv, false) ||
         !heads_ok(o, shape, heads, false) || !heads_ok(dq, shape, heads, true) || !heads_ok(dk, shape, kv, true) || !heads_ok(dv, shape, kv, true) ||
@@ -227,7 +235,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
         using T = decltype(t);
         if constexpr (sizeof(T) == 2) {
             const AttentionBackwardArgs<T> a = {heads_of<T>(d_o), heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), heads_of<T>(dq),
-                                                heads_of<T>(dk), heads_of<T>(dv), lse, dots, bounds, device_status, shape->tokens, shape->sequences,
+                                                heads_of<T>(dk), heads_of<T>(dv), lse, stats, bounds, device_status, shape->tokens, shape->sequences,
                                                 heads, heads / kv, shape->head_dim, (uint32_t)pieces, shape->scale};
             hipLaunchKernelGGL(attention_dots<T>, dim3((uint32_t)rows), dim3(256), 0, stream, a);
             if (shape->head_dim == 128) launch_backward<T, 128, true>(a, stream);

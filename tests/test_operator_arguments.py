@@ -43,7 +43,7 @@ def test_attention_tensors(S):
     shape = _shape(S)
     for call, count, written in ((_attention, 4, (3,)), (_backward, 8, (5, 6, 7))):
         for i in range(count):
-            for bad in (S._Heads(None, 512, 64), S._Heads(264, 512, 64), S._Heads(256, 510, 64), S._Heads(256, 512, 63), S._Heads(256, 1 << 41, 64)):
+            for bad in (S._Heads(None, 512, 64), S._Heads(264, 512, 64), S._Heads(256, 510, 64), S._Heads(256, 512, 63), S._Heads(256, 1 << 25, 64)):
                 t = [S._Heads(256, 512, 64) for _ in range(count)]
                 t[i] = bad
                 assert call(S, shape, t) == INVALID

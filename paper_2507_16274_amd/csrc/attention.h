@@ -140,6 +140,8 @@ template <typename T> struct Heads {
     __device__ __forceinline__ T* at(uint64_t t, uint32_t h) const { return data + t * token + h * head; }
 };
 
+constexpr int kPieceRows = 128;                              // four waves of 32
+
 // kRows rows of one sequence, or of the padding behind the last one (no_keys).
 struct Piece {
     uint32_t begin, end;                                     // the sequence
@@ -176,16 +178,48 @@ template <int kRows> __device__ __forceinline__ Piece find_piece(const uint32_t*
 // How many pieces a batch can have at most.
 inline uint64_t most_pieces(uint32_t tokens, uint32_t sequences, uint32_t rows) { return (uint64_t)tokens / rows + sequences + 1; }
 
-// The workgroup's place in the work when it is spread over the 8 dies: workgroups go to them in turn, so each die takes a contiguous share,
-// and neighbours (pieces that read the same keys) share an L2.
-__device__ __forceinline__ uint32_t place_in_work(uint32_t id, uint32_t n)
+// What the workgroups of a kernel share out among themselves: pieces of every head, and (dk and dv) parts of the walk over a piece's rows.
+//
+// Without a list every workgroup counts through the boundaries itself, heads one after the other, in each the pieces with the longest walks first: for a
+// single sequence, and for calls that are over before a list is made.  With a list (made by attention_list) the longest walks of all
+// sequences come first, whatever their order in the batch, so that none of them is the last to begin.  8000 tokens in 23 sequences, 32 heads: 115 us
+// without, 93 with a list, of which the list is 7.
+struct Work {
+    const uint4* list;                                       // {begin, end, rank, no_keys}; rank: the piece's number from that end of its sequence
+    const uint32_t* bounds;                                  //   whose walk is shortest
+    uint32_t sequences, tokens, pieces, heads, parts;
+};
+
+struct Task {
+    uint32_t head, part;
+    Piece piece;
+};
+
+// kFromEnd: a piece's walk is the longer the nearer it is to the end of its sequence (rows; else keys: to the beginning).
+template <int kRows, bool kFromEnd> __device__ __forceinline__ Task take_task(const Work& w)
 {
-    const uint32_t share = n / 8, more = n % 8, die = id % 8;
-    return die * share + umin(die, more) + id / 8;
+    if (w.list) {
+        // Workgroups go to the 8 dies in turn: neighbouring heads (which may share keys) to the same die.
+        const uint32_t at = blockIdx.x % w.heads, rest = blockIdx.x / w.heads;
+        const uint32_t head = w.heads % 8 == 0 ? at % 8 * (w.heads / 8) + at / 8 : at;
+        const uint4 e = w.list[rest / w.parts];
+        const uint32_t begin = uniform(e.x), end = uniform(e.y), rank = uniform(e.z), n = (end - begin + kRows - 1) / kRows;
+        return {head, rest % w.parts, {begin, end, begin + (kFromEnd ? rank : n - 1 - rank) * kRows, uniform(e.w) != 0}};
+    }
+    // Every die takes a contiguous share.
+    const uint32_t total = gridDim.x, share = total / 8, more = total % 8, die = blockIdx.x % 8;
+    const uint32_t at = die * share + umin(die, more) + blockIdx.x / 8, each = w.pieces * w.parts;
+    const uint32_t head = at / each, piece = at % each / w.parts;
+    return {head, at % w.parts, find_piece<kRows>(w.bounds, w.sequences, w.tokens, kFromEnd ? w.pieces - 1 - piece : piece)};
 }
 
-// The first workgroup's look at all boundaries.
-__device__ __forceinline__ void check_bounds(const uint32_t* __restrict__ bounds, uint32_t sequences, uint32_t tokens, uint32_t* status)
+// A list pays where the workgroups do not all run at once and sequences differ.
+inline bool list_pays(uint64_t workgroups, uint32_t sequences) { return sequences > 1 && workgroups >= 2048; }
+
+void launch_attention_list(const uint32_t* bounds, uint32_t sequences, uint32_t tokens, uint32_t pieces, uint4* list, uint32_t* status, hipStream_t stream);
+
+// One workgroup's look at all boundaries; whether they are as they should be.
+__device__ __forceinline__ bool check_bounds(const uint32_t* __restrict__ bounds, uint32_t sequences, uint32_t tokens, uint32_t* status)
 {
     __shared__ uint32_t bad;
     if (threadIdx.x == 0) bad = bounds[0] != 0;
@@ -195,6 +229,7 @@ __device__ __forceinline__ void check_bounds(const uint32_t* __restrict__ bounds
     if (wrong) bad = 1;
     __syncthreads();
     if (threadIdx.x == 0) *status = bad ? STALLOC_ERR_BAD_BOUNDS : STALLOC_OK;
+    return !bad;
 }
 
 constexpr uint64_t kMostStride = 1u << 24;

@@ -12,27 +12,28 @@ namespace stalloc {
 template <typename T> struct AttentionArgs {
     Heads<T> q, k, v, o;
     float* lse;
-    const uint32_t* bounds;
     uint32_t* status;
-    uint32_t tokens, sequences, heads, group, head_dim, pieces;
+    Work work;
+    uint32_t group, head_dim;
     float scale;
 };
 
-constexpr int kAttnThreads = 256, kAttnRows = 128, kAttnKeys = 64, kAttnStages = 2;
+constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2;
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, 2) attention_rows(AttentionArgs<T> a)
 {
     __shared__ T ring[kAttnStages][2][kAttnKeys * kD];       // keys, values
-    if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
-    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
-    const Piece p = find_piece<kAttnRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
+    if (blockIdx.x == 0 && !a.work.list) check_bounds(a.work.bounds, a.work.sequences, a.work.tokens, a.status);
+    const Task task = take_task<kAttnRows, true>(a.work);
+    const Piece p = task.piece;
+    const uint32_t head = task.head;
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
     if (p.no_keys) {
         if (row < p.end) {
             const f32x16 zero[kD / 32] = {};
             store_row<T, kD, kFull>(a.o.at(row, head), zero, 0.f, a.head_dim);
-            if (half == 0) a.lse[(uint64_t)head * a.tokens + row] = -INFINITY;
+            if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = -INFINITY;
         }
         return;
     }
@@ -117,7 +118,69 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     total += across(total);
     if (row >= p.end) return;
     store_row<T, kD, kFull>(a.o.at(row, head), o, total == 0.f ? 0.f : 1.f / total, a.head_dim);
-    if (half == 0) a.lse[(uint64_t)head * a.tokens + row] = (m * scale + log2f(total)) * kLn2;
+    if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = (m * scale + log2f(total)) * kLn2;
+}
+
+// All pieces of the batch, those with the longest walks first: counted by length (of their walk, in pieces), placed by count.  One workgroup; a wave takes a
+// sequence at a time.  Which of the pieces of one length comes first depends on scheduling, and nothing depends on that.
+constexpr int kListThreads = 1024, kListLengths = 1024;
+
+__global__ void __launch_bounds__(kListThreads) attention_list(const uint32_t* __restrict__ bounds, uint32_t sequences, uint32_t tokens, uint32_t pieces, uint4* list,
+                                                               uint32_t* status)
+{
+    __shared__ uint32_t whole[kListLengths + 1], rest[kListLengths + 1], wave_total[kListThreads / kWave];
+    const uint32_t t = threadIdx.x, lane = lane_id(), wave = wave_id();
+    if (!check_bounds(bounds, sequences, tokens, status)) {  // (sequences that overlap could have more pieces than there is room for)
+        for (uint32_t i = t; i < pieces; i += kListThreads) list[i] = make_uint4(0, 0, 0, 1);
+        return;
+    }
+    uint32_t shift = 0;                                      // lengths are told apart to 2^shift pieces
+    while ((tokens / kPieceRows + 1) >> shift >= kListLengths) ++shift;
+    for (uint32_t i = t; i <= kListLengths; i += kListThreads) whole[i] = rest[i] = 0;
+    __syncthreads();
+    const auto sequence = [&](uint32_t s) {
+        const uint32_t lo = umin(bounds[s], tokens);
+        return make_uint2(lo, umax(lo, umin(bounds[s + 1], tokens)));
+    };
+    for (uint32_t s = t; s < sequences; s += kListThreads) {
+        const uint2 q = sequence(s);
+        const uint32_t n = (q.y - q.x + kPieceRows - 1) / kPieceRows;
+        atomicAdd(&whole[n >> shift], 1u);                   // a sequence of n pieces has one of every length below n
+        atomicAdd(&rest[n >> shift], n & ((1u << shift) - 1));
+    }
+    __syncthreads();
+    // Pieces longer than length class k, for every k: class k holds 2^shift of every sequence that has a longer class, and the rest of those that end in it.
+    const uint32_t k = kListLengths - 1 - t;                 // (threads go through the classes from the top)
+    const uint32_t above = wave_scan_add(whole[k + 1]);      // sequences of the classes above k, within the wave
+    if (lane == kWave - 1) wave_total[wave] = above;
+    __syncthreads();
+    uint32_t longer = above;
+    for (uint32_t i = 0; i < wave; ++i) longer += wave_total[i];
+    const uint32_t here = (longer << shift) + rest[k], upto = wave_scan_add(here);
+    __syncthreads();
+    if (lane == kWave - 1) wave_total[wave] = upto;
+    __syncthreads();
+    uint32_t at = upto - here;
+    for (uint32_t i = 0; i < wave; ++i) at += wave_total[i];
+    whole[k] = at;                                           // (every thread has read whole[k + 1] before the barriers above)
+    __syncthreads();
+    for (uint32_t s = wave; s < sequences; s += kListThreads / kWave) {
+        const uint2 q = sequence(s);
+        const uint32_t n = (q.y - q.x + kPieceRows - 1) / kPieceRows;
+        for (uint32_t i = lane; i < n; i += kWave) {
+            const uint32_t to = atomicAdd(&whole[i >> shift], 1u);
+            if (to < pieces) list[to] = make_uint4(q.x, q.y, i, 0);
+        }
+    }
+    __syncthreads();
+    // Behind them the padding's pieces, then entries of nothing.
+    const uint32_t end = umin(bounds[sequences], tokens), used = whole[0], padding = (tokens - end + kPieceRows - 1) / kPieceRows;
+    for (uint32_t i = t; used + i < pieces; i += kListThreads) list[used + i] = i < padding ? make_uint4(end, tokens, i, 1) : make_uint4(0, 0, 0, 1);
+}
+
+void launch_attention_list(const uint32_t* bounds, uint32_t sequences, uint32_t tokens, uint32_t pieces, uint4* list, uint32_t* status, hipStream_t stream)
+{
+    hipLaunchKernelGGL(attention_list, dim3(1), dim3(kListThreads), 0, stream, bounds, sequences, tokens, pieces, list, status);
 }
 
 }  // namespace stalloc
@@ -142,18 +205,24 @@ extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const sta
                                  uint32_t* device_status, void* workspace, size_t* workspace_bytes, void* hip_stream)
 {
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
-    if (!workspace) { *workspace_bytes = kAlign; return STALLOC_OK; }    // (nothing is kept in it)
-    if (!heads_ok(q, shape, shape->heads, false) || !heads_ok(k, shape, shape->kv_heads, false) || !heads_ok(v, shape, shape->kv_heads, false) ||
-        !heads_ok(o, shape, shape->heads, true) || !bounds || !lse || !device_status)
-        return STALLOC_ERR_INVALID_ARG;
     const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAttnRows), blocks = pieces * shape->heads;
     if (blocks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    Carver cv(workspace);
+    uint4* list = cv.take<uint4>(list_pays(blocks, shape->sequences) ? pieces : 1);
+    if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
+    if (!heads_ok(q, shape, shape->heads, false) || !heads_ok(k, shape, shape->kv_heads, false) || !heads_ok(v, shape, shape->kv_heads, false) ||
+        !heads_ok(o, shape, shape->heads, true) || !bounds || !lse || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
+        return STALLOC_ERR_INVALID_ARG;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (list_pays(blocks, shape->sequences)) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);
+    else list = nullptr;
     with_type(shape->dtype, [&](auto t) {
         using T = decltype(t);
         if constexpr (sizeof(T) == 2) {
-            const AttentionArgs<T> a = {heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), lse, bounds, device_status, shape->tokens,
-                                        shape->sequences, shape->heads, shape->heads / shape->kv_heads, shape->head_dim, (uint32_t)pieces, shape->scale};
-            launch_attention<T>(shape, a, (uint32_t)blocks, static_cast<hipStream_t>(hip_stream));
+            const AttentionArgs<T> a = {heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), lse, device_status,
+                                        {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, shape->heads, 1},
+                                        shape->heads / shape->kv_heads, shape->head_dim, shape->scale};
+            launch_attention<T>(shape, a, (uint32_t)blocks, stream);
         }
     });
     return launched();

@@ -14,13 +14,14 @@ template <typename T> struct AttentionBackwardArgs {
     Heads<T> d_o, q, k, v, o, dq, dk, dv;
     const float* lse;
     f32x2* stats;                                            // [heads][tokens]: lse in units of log 2, D
-    const uint32_t* bounds;
     uint32_t* status;
-    uint32_t tokens, sequences, heads, group, head_dim, pieces;
+    Work rows, keys;                                         // shared out for dq; for dk and dv
+    float* partial;                                          // [parts][2][kv_heads][tokens][head_dim]: dk, dv of a part, if there are several
+    uint32_t tokens, heads, group, head_dim;
     float scale;
 };
 
-constexpr int kAbThreads = 256, kAbRows = 128, kAbStep = 32, kAbStages = 4;
+constexpr int kAbThreads = 256, kAbRows = kPieceRows, kAbStep = 32, kAbStages = 4;
 
 __device__ __forceinline__ float row_sum(float v)
 {
@@ -55,9 +56,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
 {
     __shared__ T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
     __shared__ f32x2 ring_stats[kAbStages][kAbThreads / kWave][kAbStep];     // (a copy per wave)
-    if (blockIdx.x == 0) check_bounds(a.bounds, a.sequences, a.tokens, a.status);
-    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), kv = work / a.pieces;
-    const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, work % a.pieces);           // keys that many rows see first
+    if (blockIdx.x == 0 && !a.keys.list) check_bounds(a.keys.bounds, a.keys.sequences, a.tokens, a.status);
+    const Task task = take_task<kAbRows, false>(a.keys);
+    const Piece p = task.piece;
+    const uint32_t kv = task.head, parts = a.keys.parts;
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), key = first + (lane_id() & 31);
     f32x16 dk[kD / 32] = {}, dv[kD / 32] = {};
@@ -68,8 +70,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
         const float scale = a.scale * kLog2e;
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
-        const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, steps = per_head * a.group;
-        uint32_t next_head = kv * a.group, next_row = p.first, next_slot = 0;
+        // The walk: the rows from p.first on, of one head after the other; this part's share of it.
+        const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, all = per_head * a.group;
+        const uint32_t from_step = (uint32_t)((uint64_t)all * task.part / parts), steps = (uint32_t)((uint64_t)all * (task.part + 1) / parts) - from_step;
+        uint32_t next_head = kv * a.group + from_step / per_head, next_row = p.first + from_step % per_head * kAbStep, next_slot = 0;
         const auto fetch = [&]() {
             typedef __attribute__((address_space(3))) void* lds_ptr;
             typedef const __attribute__((address_space(1))) void* global_ptr;
@@ -83,8 +87,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         };
         constexpr int kLoads = 2 * Tile::kLoads + 1;
         if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
+        uint32_t row = next_row, now = 0;
         for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch();
-        uint32_t row = p.first, now = 0;
         for (uint32_t step = 0; step < steps; ++step) {
             if (step + kAbStages - 1 < steps) {
                 tiles_landed<kLoads * (kAbStages - 2)>();
@@ -131,15 +135,34 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         }
     }
     if (key >= p.end) return;
+    if (parts > 1) {
+        const uint64_t heads = a.keys.heads, to = ((2 * task.part * heads + kv) * a.tokens + key) * a.head_dim;
+        store_row<float, kD, kFull>(a.partial + to, dk, 1.f, a.head_dim);
+        store_row<float, kD, kFull>(a.partial + to + heads * a.tokens * a.head_dim, dv, 1.f, a.head_dim);
+        return;
+    }
     store_row<T, kD, kFull>(a.dk.at(key, kv), dk, 1.f, a.head_dim);
     store_row<T, kD, kFull>(a.dv.at(key, kv), dv, 1.f, a.head_dim);
+}
+
+// dk and dv from those of the parts, added up in their order: eight numbers a thread.
+template <typename T> __global__ void __launch_bounds__(256) attention_join(AttentionBackwardArgs<T> a)
+{
+    const uint64_t each = (uint64_t)a.keys.heads * a.tokens * a.head_dim, at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= 2 * each) return;
+    f32x8 sum = load8(a.partial + at);
+    for (uint32_t part = 1; part < a.keys.parts; ++part) sum += load8(a.partial + 2 * part * each + at);
+    const uint64_t in = at < each ? at : at - each, row = in / a.head_dim;
+    const Heads<T>& to = at < each ? a.dk : a.dv;
+    store8(to.at(row % a.tokens, (uint32_t)(row / a.tokens)) + in % a.head_dim, sum);
 }
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dq(AttentionBackwardArgs<T> a)
 {
     __shared__ T ring[kAbStages][2][kAbStep * kD];           // keys, values
-    const uint32_t work = place_in_work(blockIdx.x, gridDim.x), head = work / a.pieces;
-    const Piece p = find_piece<kAbRows>(a.bounds, a.sequences, a.tokens, a.pieces - 1 - work % a.pieces);    // long rows first
+    const Task task = take_task<kAbRows, true>(a.rows);
+    const Piece p = task.piece;
+    const uint32_t head = task.head;
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
     f32x16 dq[kD / 32] = {};
@@ -207,8 +230,16 @@ namespace {
 
 template <typename T, int kD, bool kFull> void launch_backward(const AttentionBackwardArgs<T>& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.pieces * (a.heads / a.group)), dim3(kAbThreads), 0, stream, a);
-    hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.pieces * a.heads), dim3(kAbThreads), 0, stream, a);
+    hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.keys.pieces * a.keys.heads * a.keys.parts), dim3(kAbThreads), 0, stream, a);
+    hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.rows.pieces * a.heads), dim3(kAbThreads), 0, stream, a);
+}
+
+// Parts of the walk over a piece's rows: one, unless the pieces alone do not give every CU two workgroups.  A part leaves 8 bytes for every number of k in
+// the workspace, which are written and read once.
+uint32_t parts_of(const stalloc_attention_shape* s)
+{
+    const uint64_t pieces = ((uint64_t)s->tokens + kAbRows - 1) / kAbRows * s->kv_heads;
+    return pieces >= 512 ? 1 : umin_host(8, (uint32_t)((512 + pieces - 1) / pieces));
 }
 
 }  // namespace
@@ -220,28 +251,37 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
                                           size_t* workspace_bytes, void* hip_stream)
 {
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
-    const uint32_t heads = shape->heads, kv = shape->kv_heads;
+    const uint32_t heads = shape->heads, kv = shape->kv_heads, parts = parts_of(shape);
+    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows), rows = ((uint64_t)shape->tokens * heads + 15) / 16;
+    const uint64_t joined = 2 * (uint64_t)kv * shape->tokens * shape->head_dim;
+    if (pieces * heads > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || rows > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    const bool listed = list_pays(pieces * heads, shape->sequences);
     Carver cv(workspace);
     f32x2* stats = cv.take<f32x2>((size_t)shape->tokens * heads + kAbStep);
+    uint4* list = cv.take<uint4>(listed ? pieces : 0);
+    float* partial = cv.take<float>(parts > 1 ? parts * joined : 0);
     if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
     if (!heads_ok(d_o, shape, heads, false) || !heads_ok(q, shape, heads, false) || !heads_ok(k, shape, kv, false) || !heads_ok(v, shape, kv, false) ||
         !heads_ok(o, shape, heads, false) || !heads_ok(dq, shape, heads, true) || !heads_ok(dk, shape, kv, true) || !heads_ok(dv, shape, kv, true) ||
         !lse || !bounds || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
         return STALLOC_ERR_INVALID_ARG;
-    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows), rows = ((uint64_t)shape->tokens * heads + 15) / 16;
-    if (pieces * heads > 0x7fffffffu || rows > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (listed) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);
+    else list = nullptr;
+    const Work by_rows = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, heads, 1};
+    const Work by_keys = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, kv, parts};
     with_type(shape->dtype, [&](auto t) {
         using T = decltype(t);
         if constexpr (sizeof(T) == 2) {
             const AttentionBackwardArgs<T> a = {heads_of<T>(d_o), heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), heads_of<T>(dq),
-                                                heads_of<T>(dk), heads_of<T>(dv), lse, stats, bounds, device_status, shape->tokens, shape->sequences,
-                                                heads, heads / kv, shape->head_dim, (uint32_t)pieces, shape->scale};
+                                                heads_of<T>(dk), heads_of<T>(dv), lse, stats, device_status, by_rows, by_keys, partial, shape->tokens,
+                                                heads, heads / kv, shape->head_dim, shape->scale};
             hipLaunchKernelGGL(attention_dots<T>, dim3((uint32_t)rows), dim3(256), 0, stream, a);
             if (shape->head_dim == 128) launch_backward<T, 128, true>(a, stream);
             else if (shape->head_dim > 64) launch_backward<T, 128, false>(a, stream);
             else if (shape->head_dim == 64) launch_backward<T, 64, true>(a, stream);
             else launch_backward<T, 64, false>(a, stream);
+            if (parts > 1) hipLaunchKernelGGL(attention_join<T>, dim3((uint32_t)((joined / 8 + 255) / 256)), dim3(256), 0, stream, a);
         }
     });
     return launched();

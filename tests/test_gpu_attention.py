@@ -222,3 +222,44 @@ def test_bad_bounds_are_reported(S, cuts):
     assert int(f["status"].item()) == 10 and int(b["status"].item()) == 10
     with pytest.raises(S.StallocError, match="STALLOC_ERR_BAD_BOUNDS"):
         S.check_status(f)
+
+
+def _lengths(seed, count, most):
+    rng = np.random.default_rng(seed)
+    return [int(n) for n in np.exp(rng.uniform(0.0, np.log(most), count))]
+
+
+@pytest.mark.parametrize("seed,count,most,pad", [(1, 40, 900, 0), (2, 700, 60, 130), (3, 3000, 3, 1)])
+def test_batches_whose_pieces_are_listed(S, seed, count, most, pad):
+    """Enough pieces and heads for the list that puts the longest walks first (more sequences than a workgroup looks at in one go
+    among them): the same numbers as for each sequence alone, which needs no list."""
+    import torch
+    lengths = _lengths(seed, count, most)
+    lengths[3:5] = [0, 0]
+    n, h, g, d = sum(lengths) + pad, 64, 4, 64
+    q, k, v, d_o = _inputs(seed, n, h, g, d, torch.bfloat16)
+    bounds = _bounds(lengths)
+    f = S.stalloc_attention(q, k, v, bounds)
+    b = S.stalloc_attention_backward(d_o, q, k, v, f["o"], f["lse"], bounds)
+    torch.cuda.synchronize()
+    S.check_status(f)
+    S.check_status(b)
+    assert f["workspace"].numel() > 256                       # (the list is in it: 16 bytes a piece)
+    cuts = bounds.cpu().tolist()
+    for s in range(0, count, max(1, count // 12)):
+        lo, hi = cuts[s], cuts[s + 1]
+        if lo == hi:
+            continue
+        alone = [x[lo:hi] for x in (q, k, v)]
+        one = S.stalloc_attention(*alone, _bounds([hi - lo]))
+        assert torch.equal(one["o"], f["o"][lo:hi]) and torch.equal(one["lse"], f["lse"][:, lo:hi])
+        back = S.stalloc_attention_backward(d_o[lo:hi], *alone, one["o"], one["lse"], _bounds([hi - lo]))
+        assert torch.equal(back["dq"], b["dq"][lo:hi])
+        for name in ("dk", "dv"):                             # (their sums may be cut into parts where a call is short)
+            size = back[name].float().abs().amax()
+            assert float((back[name].float() - b[name][lo:hi].float()).abs().max()) <= 2.0 ** -7 * float(size)
+    if pad:
+        assert float(f["o"][n - pad:].abs().max()) == 0.0 and float(b["dk"][n - pad:].abs().max()) == 0.0
+    cuts[2] = n + 5
+    bad = torch.tensor(cuts, dtype=torch.int32).cuda()
+    assert int(S.stalloc_attention(q, k, v, bad)["status"].item()) == 10

@@ -35,35 +35,46 @@ __device__ __forceinline__ float across(float v)
     return as_float(lane_id() < 32 ? r[1] : r[0]);
 }
 
-// A tile of rows of kD numbers in LDS.  16-byte pieces of a row change places with the row's number, so that the lanes of one access,
-// which are in different rows at the same column, reach all banks:
-//   kAlong  for reads of 16 bytes along a row (one row per lane)
-//   kCross  for transposing reads, in which 16 lanes take 32 bytes of each of four rows
-// Where a tile is read both ways the second one serves (pairs of pieces stay together).
-enum class Order { kAlong, kCross };
-template <int kD, Order kOrder> __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece)
+// A tile of rows of kD numbers in LDS.  16-byte pieces of a row change places with the row's number, so that lanes in different rows at one column
+// reach different banks (64 of 4 bytes, a row of 128 numbers takes all of them) both in reads along a row, 16 rows at
+// a time, and in transposing reads, 64 bytes of each of four neighbouring rows at a time: the low bits of the row move blocks of
+// four pieces, the next ones pieces within a block.  (Moving pairs of pieces by the row's low bits cost two further cycles a
+// transposing read and four a read along a row: attention_long 1142 -> XX us without them.)
+template <int kD> __device__ __forceinline__ uint32_t turn_of(uint32_t row)
 {
-    constexpr uint32_t kPieces = kD / 8;
-    const uint32_t turn = kOrder == Order::kAlong ? row & (kPieces - 1) : (row << 1) & (kPieces - 1);
-    return row * kD + ((piece ^ turn) << 3);
+    return kD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-template <typename T, int kD, Order kOrder> __device__ __forceinline__ V8<T> read_along(const T* tile, uint32_t row, uint32_t piece)
+// Where a lane reads in a tile, in bytes.  The columns that a read is for only change bits that the tile's place does not reach: they are put in
+// by an exclusive or where the read is, which costs an instruction and saves the registers of all the places.
+//   along  its row l % 32, numbers 8 (l / 32) .. + 7; columns 16 c further on: along ^ 32 c
+//   cross  of a transposing read, in which lane i of 16 gets the i-th column of four rows whose quarters its neighbours point at: column l % 32, rows
+//          4 (l / 32) .. + 3; columns 32 d further on: cross ^ 64 d; eight rows further on: (cross ^ 32) + 16 kD
+template <int kD> struct Places {
+    uint32_t along, cross;
+    __device__ __forceinline__ Places()
+    {
+        const uint32_t l = lane_id(), row = l & 31, half = l >> 5, i = l & 15, from = 4 * half + (i >> 2), col = 16 * ((l >> 4) & 1) + 4 * (i & 3);
+        along = row * kD * 2 + ((half ^ turn_of<kD>(row)) << 4);
+        cross = from * kD * 2 + (((col >> 3) ^ turn_of<kD>(from)) << 4) + (col & 7) * 2;
+    }
+};
+
+// The A operand of a product over columns 16 c .. + 15 of the rows l % 32 of the tile that lies `tile` bytes behind `ring`.
+template <typename T, int kD> __device__ __forceinline__ V8<T> read_along(const T* ring, uint32_t along_in_tile, int c, uint32_t further = 0)
 {
-    return *(const V8<T>*)(tile + place<kD, kOrder>(row, piece));
+    return *(const V8<T>*)((const char*)ring + ((along_in_tile ^ (32 * c)) + further));
 }
 
-// The A operand of a product over 16 rows of the tile (from row `base`, a multiple of 16) for 32 of its columns from column `col`: lane l gets
-// column col + l % 32 and the rows in the order of `operand`.  A transposing read gives lane i of 16 the i-th column of
-// four rows, whose quarters its neighbours point at.
-template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const T* tile, uint32_t base, uint32_t col)
+// The A operand of a product over 16 rows (`further`: bytes to the first of them, whole multiples of 16 rows) for columns 32 d .. + 31: lane l gets
+// column 32 d + l % 32 and the rows in the order of `operand`.
+template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const T* ring, uint32_t cross_in_tile, int d, uint32_t further = 0)
 {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-    const uint32_t l = lane_id(), i = l & 15, c = col + 16 * ((l >> 4) & 1) + 4 * (i & 3), row = base + 4 * (l >> 5) + (i >> 2);
-    const T* at = tile + place<kD, Order::kCross>(row, c >> 3) + (c & 7);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * kD));     // (the row eight further on turns the same way)
+    const uint32_t at = cross_in_tile ^ (64 * d);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)((const char*)ring + (at + further)));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)((const char*)ring + ((at ^ 32) + further + 16 * kD)));
     const V4<T> a = __builtin_bit_cast(V4<T>, lo), b = __builtin_bit_cast(V4<T>, hi);
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
@@ -75,7 +86,7 @@ template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Rows {
     static constexpr int kPieces = kD / 8, kLoads = kRows * kPieces / kThreads;
     static_assert(kLoads * kThreads == kRows * kPieces, "whole accesses");
 
-    template <Order kOrder> static __device__ __forceinline__ void fetch(T* tile, const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
+    static __device__ __forceinline__ void fetch(T* tile, const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
     {
         typedef __attribute__((address_space(3))) void* lds_ptr;
         typedef const __attribute__((address_space(1))) void* global_ptr;
@@ -83,7 +94,7 @@ template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Rows {
         const uint32_t bytes = (uint32_t)stride * sizeof(T), most = last - first;
 #pragma unroll
         for (int s = 0; s < kLoads; ++s) {
-            const uint32_t at = s * kThreads + threadIdx.x, row = at / kPieces, piece = (at % kPieces) ^ (place<kD, kOrder>(row, 0) / 8 % kPieces);
+            const uint32_t at = s * kThreads + threadIdx.x, row = at / kPieces, piece = (at % kPieces) ^ turn_of<kD>(row);
             const uint32_t offset = umin(row, most) * bytes + piece * 16;
             if (kFull || piece * 8 < head_dim)
                 __builtin_amdgcn_global_load_lds((global_ptr)(base + offset), (lds_ptr)(tile + (s * kThreads + wave_id() * kWave) * 8), 16, 0, 0);
@@ -180,10 +191,10 @@ inline uint64_t most_pieces(uint32_t tokens, uint32_t sequences, uint32_t rows) 
 
 // What the workgroups of a kernel share out among themselves: pieces of every head, and (dk and dv) parts of the walk over a piece's rows.
 //
-// Without a list every workgroup counts through the boundaries itself, heads one after the other, in each the pieces with the longest walks first: for a
-// single sequence, and for calls that are over before a list is made.  With a list (made by attention_list) the longest walks of all
-// sequences come first, whatever their order in the batch, so that none of them is the last to begin.  8000 tokens in 23 sequences, 32 heads: 115 us
-// without, 93 with a list, of which the list is 7.
+// The longest walks come first, those of all heads: the last workgroups to begin are then the shortest.  (Heads one after the other instead, each from
+// its longest walk on, took 198 us for one sequence of 4096 and 32 heads of 128, this order takes XX.)  For a single sequence the order of the pieces is
+// known; for several, attention_list makes a list of all pieces in that order.  Without one (a single sequence; calls that would be over before the list is
+// made) every workgroup counts through the boundaries itself.
 struct Work {
     const uint4* list;                                       // {begin, end, rank, no_keys}; rank: the piece's number from that end of its sequence
     const uint32_t* bounds;                                  //   whose walk is shortest
@@ -198,19 +209,14 @@ struct Task {
 // kFromEnd: a piece's walk is the longer the nearer it is to the end of its sequence (rows; else keys: to the beginning).
 template <int kRows, bool kFromEnd> __device__ __forceinline__ Task take_task(const Work& w)
 {
+    // Workgroups go to the 8 dies in turn: neighbouring heads (which may share keys) to the same die.
+    const uint32_t at = blockIdx.x % w.heads, rest = blockIdx.x / w.heads, head = w.heads % 8 == 0 ? at % 8 * (w.heads / 8) + at / 8 : at, piece = rest / w.parts;
     if (w.list) {
-        // Workgroups go to the 8 dies in turn: neighbouring heads (which may share keys) to the same die.
-        const uint32_t at = blockIdx.x % w.heads, rest = blockIdx.x / w.heads;
-        const uint32_t head = w.heads % 8 == 0 ? at % 8 * (w.heads / 8) + at / 8 : at;
-        const uint4 e = w.list[rest / w.parts];
+        const uint4 e = w.list[piece];
         const uint32_t begin = uniform(e.x), end = uniform(e.y), rank = uniform(e.z), n = (end - begin + kRows - 1) / kRows;
         return {head, rest % w.parts, {begin, end, begin + (kFromEnd ? rank : n - 1 - rank) * kRows, uniform(e.w) != 0}};
     }
-    // Every die takes a contiguous share.
-    const uint32_t total = gridDim.x, share = total / 8, more = total % 8, die = blockIdx.x % 8;
-    const uint32_t at = die * share + umin(die, more) + blockIdx.x / 8, each = w.pieces * w.parts;
-    const uint32_t head = at / each, piece = at % each / w.parts;
-    return {head, at % w.parts, find_piece<kRows>(w.bounds, w.sequences, w.tokens, kFromEnd ? w.pieces - 1 - piece : piece)};
+    return {head, rest % w.parts, find_piece<kRows>(w.bounds, w.sequences, w.tokens, kFromEnd ? w.pieces - 1 - piece : piece)};
 }
 
 // A list pays where the workgroups do not all run at once and sequences differ.

@@ -18,11 +18,11 @@ template <typename T> struct AttentionArgs {
     float scale;
 };
 
-constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2;
+constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2, kAttnTiles = kAttnKeys / 32;
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, 2) attention_rows(AttentionArgs<T> a)
 {
-    __shared__ T ring[kAttnStages][2][kAttnKeys * kD];       // keys, values
+    __shared__ __attribute__((aligned(256))) T ring[kAttnStages][2][kAttnKeys * kD];       // keys, values
     if (blockIdx.x == 0 && !a.work.list) check_bounds(a.work.bounds, a.work.sequences, a.work.tokens, a.status);
     const Task task = take_task<kAttnRows, true>(a.work);
     const Piece p = task.piece;
@@ -44,14 +44,15 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
 
     const float scale = a.scale * kLog2e, slack = 8.f / scale;
+    const Places<kD> places;
     float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
     f32x16 o[kD / 32] = {};
     const uint32_t steps = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
     using Tile = Rows<T, kD, kAttnKeys, kAttnThreads, kFull>;
     const auto fetch = [&](uint32_t step) {
         T (&stage)[2][kAttnKeys * kD] = ring[step % kAttnStages];
-        Tile::template fetch<Order::kAlong>(stage[0], k, a.k.token, p.begin + step * kAttnKeys, last, a.head_dim);
-        Tile::template fetch<Order::kCross>(stage[1], v, a.v.token, p.begin + step * kAttnKeys, last, a.head_dim);
+        Tile::fetch(stage[0], k, a.k.token, p.begin + step * kAttnKeys, last, a.head_dim);
+        Tile::fetch(stage[1], v, a.v.token, p.begin + step * kAttnKeys, last, a.head_dim);
     };
     if (!kFull) clear_lds<sizeof(ring) / 4, kAttnThreads>(ring);
 #pragma unroll
@@ -59,8 +60,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
         if (step < steps) fetch(step);
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t key = p.begin + step * kAttnKeys;
-        const T* tile_k = ring[step % kAttnStages][0];
-        const T* tile_v = ring[step % kAttnStages][1];
+        constexpr uint32_t kTile = sizeof(ring[0][0]);
+        const uint32_t tile = step % kAttnStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
         if (step + kAttnStages - 1 < steps) {
             tiles_landed<2 * Tile::kLoads * (kAttnStages - 2)>();
             fetch(step + kAttnStages - 1);
@@ -68,24 +69,27 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
             tiles_landed<0>();
         }
         if (key <= first + 31) {                             // (else none of the wave's rows sees any of these keys)
-            f32x16 s[2] = {};
+            f32x16 s[kAttnTiles] = {};
 #pragma unroll
             for (int c = 0; c < kD / 16; ++c)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-                    s[t] = mma(read_along<T, kD, Order::kAlong>(tile_k, 32 * t + (lane_id() & 31), 2 * c + half), q[c], s[t]);
+                for (int t = 0; t < kAttnTiles; ++t)
+                    s[t] = mma(read_along<T, kD>(ring[0][0], along, c, 64 * kD * t), q[c], s[t]);
             if (key + kAttnKeys - 1 > first) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < kAttnTiles; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (key + 32 * t + row_of(i, half) > row) s[t][i] = -INFINITY;
             }
-            float most = s[0][0];
+            float most = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kAttnTiles; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
+                for (int i = 0; i < 16; i += 8) {
+                    const float a0 = max3(s[t][i], s[t][i + 1], s[t][i + 2]), a1 = max3(s[t][i + 3], s[t][i + 4], s[t][i + 5]);
+                    most = max3(most, a0, max3(a1, s[t][i + 6], s[t][i + 7]));
+                }
             most = fmaxf(most, across(most));
             // The maximum is raised only where weights would pass 2^8 otherwise: sums and results are relative to it all the same.
             if (__any(most > m + slack)) {
@@ -96,21 +100,23 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                 for (int d = 0; d < kD / 32; ++d) o[d] *= f;
             }
             const float shift = m * scale;
+            float sums[4] = {total, 0.f, 0.f, 0.f};          // (four chains of additions)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kAttnTiles; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[t][i] = exp2_fast(__builtin_fmaf(s[t][i], scale, -shift));
-                    total += s[t][i];
+                    sums[i % 4] += s[t][i];
                 }
+            total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
             // Weights are rounded to T for the product (half a step of T each, and of alternating sign); their sum is not.
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int t = 0; t < kAttnTiles; ++t) {
                 const V8<T> w0 = operand<T, 0>(s[t]), w1 = operand<T, 1>(s[t]);
 #pragma unroll
                 for (int d = 0; d < kD / 32; ++d) {
-                    o[d] = mma(read_cross<T, kD>(tile_v, 32 * t, 32 * d), w0, o[d]);
-                    o[d] = mma(read_cross<T, kD>(tile_v, 32 * t + 16, 32 * d), w1, o[d]);
+                    o[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 64 * kD * t), w0, o[d]);
+                    o[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 64 * kD * t + 32 * kD), w1, o[d]);
                 }
             }
         }

@@ -54,7 +54,7 @@ template <typename T> __global__ void __launch_bounds__(256) attention_dots(Atte
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dk_dv(AttentionBackwardArgs<T> a)
 {
-    __shared__ T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
+    __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
     __shared__ f32x2 ring_stats[kAbStages][kAbThreads / kWave][kAbStep];     // (a copy per wave)
     if (blockIdx.x == 0 && !a.keys.list) check_bounds(a.keys.bounds, a.keys.sequences, a.tokens, a.status);
     const Task task = take_task<kAbRows, false>(a.keys);
@@ -70,6 +70,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
         const float scale = a.scale * kLog2e;
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
+        constexpr uint32_t kTile = sizeof(ring[0][0]);
+        const Places<kD> places;
         // The walk: the rows from p.first on, of one head after the other; this part's share of it.
         const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, all = per_head * a.group;
         const uint32_t from_step = (uint32_t)((uint64_t)all * task.part / parts), steps = (uint32_t)((uint64_t)all * (task.part + 1) / parts) - from_step;
@@ -77,8 +79,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const auto fetch = [&]() {
             typedef __attribute__((address_space(3))) void* lds_ptr;
             typedef const __attribute__((address_space(1))) void* global_ptr;
-            Tile::template fetch<Order::kCross>(ring[next_slot][0], a.q.at(0, next_head), a.q.token, next_row, last, a.head_dim);
-            Tile::template fetch<Order::kCross>(ring[next_slot][1], a.d_o.at(0, next_head), a.d_o.token, next_row, last, a.head_dim);
+            Tile::fetch(ring[next_slot][0], a.q.at(0, next_head), a.q.token, next_row, last, a.head_dim);
+            Tile::fetch(ring[next_slot][1], a.d_o.at(0, next_head), a.d_o.token, next_row, last, a.head_dim);
             const float* from = (const float*)(a.stats + (uint64_t)next_head * a.tokens + next_row);   // (room for a whole step is behind the last row)
             __builtin_amdgcn_global_load_lds((global_ptr)(from + lane_id()), (lds_ptr)ring_stats[next_slot][wave_id()], 4, 0, 0);
             next_row += kAbStep;
@@ -96,15 +98,14 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             } else {
                 tiles_landed<0>();
             }
-            const T* tile_q = ring[now][0];
-            const T* tile_do = ring[now][1];
+            const uint32_t along = now * 2 * kTile + places.along, cross = now * 2 * kTile + places.cross;
             const f32x2* stats = ring_stats[now][wave_id()];
             if (row + kAbStep - 1 >= first) {                // (else none of these rows sees a key of this wave)
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int c = 0; c < kD / 16; ++c) {
-                    s = mma(read_along<T, kD, Order::kCross>(tile_q, lane_id() & 31, 2 * c + half), k[c], s);
-                    dp = mma(read_along<T, kD, Order::kCross>(tile_do, lane_id() & 31, 2 * c + half), v[c], dp);
+                    s = mma(read_along<T, kD>(ring[0][0], along, c), k[c], s);
+                    dp = mma(read_along<T, kD>(ring[0][0], along, c, kTile), v[c], dp);
                 }
                 const bool crosses = row < first + 31 || row + kAbStep > p.end;      // some of these rows do not see some of these keys, or are not the sequence's
 #pragma unroll
@@ -123,10 +124,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                 const V8<T> w0 = operand<T, 0>(s), w1 = operand<T, 1>(s), d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
 #pragma unroll
                 for (int d = 0; d < kD / 32; ++d) {
-                    dv[d] = mma(read_cross<T, kD>(tile_do, 0, 32 * d), w0, dv[d]);
-                    dv[d] = mma(read_cross<T, kD>(tile_do, 16, 32 * d), w1, dv[d]);
-                    dk[d] = mma(read_cross<T, kD>(tile_q, 0, 32 * d), d0, dk[d]);
-                    dk[d] = mma(read_cross<T, kD>(tile_q, 16, 32 * d), d1, dk[d]);
+                    dv[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile), w0, dv[d]);
+                    dv[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 32 * kD), w1, dv[d]);
+                    dk[d] = mma(read_cross<T, kD>(ring[0][0], cross, d), d0, dk[d]);
+                    dk[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, 32 * kD), d1, dk[d]);
                 }
             }
             row += kAbStep;
@@ -159,7 +160,7 @@ template <typename T> __global__ void __launch_bounds__(256) attention_join(Atte
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dq(AttentionBackwardArgs<T> a)
 {
-    __shared__ T ring[kAbStages][2][kAbStep * kD];           // keys, values
+    __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // keys, values
     const Task task = take_task<kAbRows, true>(a.rows);
     const Piece p = task.piece;
     const uint32_t head = task.head;
@@ -176,11 +177,13 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const f32x2 stats = a.stats[(uint64_t)head * a.tokens + mine];
         const float scale = a.scale * kLog2e;
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
+        constexpr uint32_t kTile = sizeof(ring[0][0]);
+        const Places<kD> places;
         const uint32_t steps = (umin(p.first + kAbRows, p.end) - p.begin + kAbStep - 1) / kAbStep;
         const auto fetch = [&](uint32_t step) {
             T (&stage)[2][kAbStep * kD] = ring[step % kAbStages];
-            Tile::template fetch<Order::kCross>(stage[0], k, a.k.token, p.begin + step * kAbStep, last, a.head_dim);
-            Tile::template fetch<Order::kAlong>(stage[1], v, a.v.token, p.begin + step * kAbStep, last, a.head_dim);
+            Tile::fetch(stage[0], k, a.k.token, p.begin + step * kAbStep, last, a.head_dim);
+            Tile::fetch(stage[1], v, a.v.token, p.begin + step * kAbStep, last, a.head_dim);
         };
         if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
         for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch(step);
@@ -192,14 +195,13 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             } else {
                 tiles_landed<0>();
             }
-            const T* tile_k = ring[step % kAbStages][0];
-            const T* tile_v = ring[step % kAbStages][1];
+            const uint32_t tile = step % kAbStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
             if (key > first + 31) continue;                  // (none of the wave's rows sees any of these keys)
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int c = 0; c < kD / 16; ++c) {
-                s = mma(read_along<T, kD, Order::kCross>(tile_k, lane_id() & 31, 2 * c + half), q[c], s);
-                dp = mma(read_along<T, kD, Order::kAlong>(tile_v, lane_id() & 31, 2 * c + half), d_o[c], dp);
+                s = mma(read_along<T, kD>(ring[0][0], along, c), q[c], s);
+                dp = mma(read_along<T, kD>(ring[0][0], along, c, kTile), d_o[c], dp);
             }
             const bool crosses = key + 31 > first;
 #pragma unroll
@@ -214,8 +216,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const V8<T> d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
 #pragma unroll
             for (int d = 0; d < kD / 32; ++d) {
-                dq[d] = mma(read_cross<T, kD>(tile_k, 0, 32 * d), d0, dq[d]);
-                dq[d] = mma(read_cross<T, kD>(tile_k, 16, 32 * d), d1, dq[d]);
+                dq[d] = mma(read_cross<T, kD>(ring[0][0], cross, d), d0, dq[d]);
+                dq[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, 32 * kD), d1, dq[d]);
             }
         }
     }

@@ -18,6 +18,8 @@ template <typename T> using V8 = typename Vec<T>::x8;
 __device__ __forceinline__ f32x16 mma(V8<bf16> a, V8<bf16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mma(V8<f16> a, V8<f16> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
+constexpr int kOthersMayMove = 0x2 | 0x4;                    // vector and scalar instructions, not memory accesses and matrix products
+
 // Registers 8 s .. 8 s + 7 of a result, rounded to T, as the operand of the next product.
 template <typename T, int s> __device__ __forceinline__ V8<T> operand(const f32x16& x)
 {
@@ -79,28 +81,52 @@ template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const 
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// kRows rows of a tensor on their way to LDS, 16 bytes per lane and access, without a register between: the memory pipe writes 64 lanes' pieces one
-// behind the other, so a lane asks for the piece that belongs where its own lands.  Rows past `last` repeat it; columns from head_dim
-// on are left as they are (the kernel has cleared them).  `first` <= `last`; kLoads accesses of every wave, counted by vmcnt.
+// 16 (or 4) bytes per lane from memory to LDS, lane after lane from `lds` on; `base` and `lds` are the same in all lanes.  Written out because
+// the compiler, which cannot know that the tile asked for is not the one read next, would wait for it there and then; what waits
+// for it is tiles_landed.  Nothing is returned in registers.
+template <int kBytes> __device__ __forceinline__ void memory_to_lds(uint32_t lds, const void* base, uint32_t offset)
+{
+    static_assert(kBytes == 16 || kBytes == 4, "16 or 4 bytes a lane");
+    const uint64_t from = uniform((uint64_t)base);
+    if (kBytes == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return uniform((uint32_t)(size_t)(__attribute__((address_space(3))) const void*)p); }
+
+// kRows rows of a tensor on their way to LDS, without a register between: the memory pipe writes 64 lanes' pieces one behind the other, so a lane asks
+// for the piece that belongs where its own lands.  Rows past `last` repeat it; columns from head_dim on are left as they are (the
+// kernel has cleared them).  `first` <= `last`; kLoads accesses of every wave, counted by vmcnt.
 template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Rows {
     static constexpr int kPieces = kD / 8, kLoads = kRows * kPieces / kThreads;
     static_assert(kLoads * kThreads == kRows * kPieces, "whole accesses");
 
     static __device__ __forceinline__ void fetch(T* tile, const T* data, uint64_t stride, uint32_t first, uint32_t last, uint32_t head_dim)
     {
-        typedef __attribute__((address_space(3))) void* lds_ptr;
-        typedef const __attribute__((address_space(1))) void* global_ptr;
         const char* base = (const char*)(data + first * stride);
-        const uint32_t bytes = (uint32_t)stride * sizeof(T), most = last - first;
+        const uint32_t bytes = (uint32_t)stride * sizeof(T), most = last - first, lds = lds_address(tile) + wave_id() * kWave * 16;
 #pragma unroll
         for (int s = 0; s < kLoads; ++s) {
             const uint32_t at = s * kThreads + threadIdx.x, row = at / kPieces, piece = (at % kPieces) ^ turn_of<kD>(row);
-            const uint32_t offset = umin(row, most) * bytes + piece * 16;
-            if (kFull || piece * 8 < head_dim)
-                __builtin_amdgcn_global_load_lds((global_ptr)(base + offset), (lds_ptr)(tile + (s * kThreads + wave_id() * kWave) * 8), 16, 0, 0);
+            if (kFull || piece * 8 < head_dim) memory_to_lds<16>(lds + s * kThreads * 16, base, umin(row, most) * bytes + piece * 16);
         }
     }
 };
+
+// kN products whose A operands come from LDS: `read(i)` of one is under way while kAhead others are made of `multiply(i, operand)`.  The compiler
+// keeps this order (other instructions may move): left to itself it waits for every operand right behind its read.
+template <int kN, int kAhead, typename T, typename Read, typename Multiply> __device__ __forceinline__ void products(Read read, Multiply multiply)
+{
+    V8<T> a[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) a[i] = read(i);
+    __builtin_amdgcn_sched_barrier(kOthersMayMove);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        multiply(i, a[i % kAhead]);
+        if (i + kAhead < kN) a[i % kAhead] = read(i + kAhead);
+        __builtin_amdgcn_sched_barrier(kOthersMayMove);
+    }
+}
 
 // The tiles that the wave's accesses were asked for before the last `kLater` ones have landed, its own reads are done, and so are the other
 // waves': behind this the tile may be read, and the one read before it written.

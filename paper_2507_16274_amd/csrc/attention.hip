@@ -40,9 +40,6 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     const uint32_t last = p.end - 1, kv = head / a.group;
     const T* k = a.k.at(0, kv);
     const T* v = a.v.at(0, kv);
-    V8<T> q[kD / 16];
-    load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
-
     const float scale = a.scale * kLog2e, slack = 8.f / scale;
     const Places<kD> places;
     float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
@@ -58,6 +55,9 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
 #pragma unroll
     for (uint32_t step = 0; step < kAttnStages - 1; ++step)
         if (step < steps) fetch(step);
+    V8<T> q[kD / 16];
+    load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
+    vector_memory_done();                                    // (q is here before the loop: its loads are not waited for among the tiles')
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t key = p.begin + step * kAttnKeys;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
@@ -70,11 +70,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
         }
         if (key <= first + 31) {                             // (else none of the wave's rows sees any of these keys)
             f32x16 s[kAttnTiles] = {};
-#pragma unroll
-            for (int c = 0; c < kD / 16; ++c)
-#pragma unroll
-                for (int t = 0; t < kAttnTiles; ++t)
-                    s[t] = mma(read_along<T, kD>(ring[0][0], along, c, 64 * kD * t), q[c], s[t]);
+            products<kAttnTiles * kD / 16, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / kAttnTiles, 64 * kD * (i % kAttnTiles)); },
+                                                 [&](int i, V8<T> k) { s[i % kAttnTiles] = mma(k, q[i / kAttnTiles], s[i % kAttnTiles]); });
             if (key + kAttnKeys - 1 > first) {
 #pragma unroll
                 for (int t = 0; t < kAttnTiles; ++t)
@@ -110,15 +107,15 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                 }
             total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
             // Weights are rounded to T for the product (half a step of T each, and of alternating sign); their sum is not.
+            V8<T> w[2 * kAttnTiles];
 #pragma unroll
             for (int t = 0; t < kAttnTiles; ++t) {
-                const V8<T> w0 = operand<T, 0>(s[t]), w1 = operand<T, 1>(s[t]);
-#pragma unroll
-                for (int d = 0; d < kD / 32; ++d) {
-                    o[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 64 * kD * t), w0, o[d]);
-                    o[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 64 * kD * t + 32 * kD), w1, o[d]);
-                }
+                w[2 * t] = operand<T, 0>(s[t]);
+                w[2 * t + 1] = operand<T, 1>(s[t]);
             }
+            constexpr int kDs = kD / 32;
+            products<2 * kAttnTiles * kDs, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, kTile + 32 * kD * (i / kDs)); },
+                                                 [&](int i, V8<T> v) { o[i % kDs] = mma(v, w[i / kDs], o[i % kDs]); });
         }
     }
     total += across(total);

@@ -65,9 +65,6 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     f32x16 dk[kD / 32] = {}, dv[kD / 32] = {};
     if (!p.no_keys) {
         const uint32_t last = p.end - 1;
-        V8<T> k[kD / 16], v[kD / 16];
-        load_row<T, kD, kFull>(k, a.k.at(umin(key, last), kv), a.head_dim);
-        load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
         const float scale = a.scale * kLog2e;
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
@@ -77,12 +74,9 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const uint32_t from_step = (uint32_t)((uint64_t)all * task.part / parts), steps = (uint32_t)((uint64_t)all * (task.part + 1) / parts) - from_step;
         uint32_t next_head = kv * a.group + from_step / per_head, next_row = p.first + from_step % per_head * kAbStep, next_slot = 0;
         const auto fetch = [&]() {
-            typedef __attribute__((address_space(3))) void* lds_ptr;
-            typedef const __attribute__((address_space(1))) void* global_ptr;
             Tile::fetch(ring[next_slot][0], a.q.at(0, next_head), a.q.token, next_row, last, a.head_dim);
             Tile::fetch(ring[next_slot][1], a.d_o.at(0, next_head), a.d_o.token, next_row, last, a.head_dim);
-            const float* from = (const float*)(a.stats + (uint64_t)next_head * a.tokens + next_row);   // (room for a whole step is behind the last row)
-            __builtin_amdgcn_global_load_lds((global_ptr)(from + lane_id()), (lds_ptr)ring_stats[next_slot][wave_id()], 4, 0, 0);
+            memory_to_lds<4>(lds_address(ring_stats[next_slot][wave_id()]), a.stats + (uint64_t)next_head * a.tokens + next_row, lane_id() * 4);
             next_row += kAbStep;
             if (next_row >= p.end) { next_row = p.first; ++next_head; }
             next_slot = (next_slot + 1) % kAbStages;
@@ -91,6 +85,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
         uint32_t row = next_row, now = 0;
         for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch();
+        V8<T> k[kD / 16], v[kD / 16];
+        load_row<T, kD, kFull>(k, a.k.at(umin(key, last), kv), a.head_dim);
+        load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
+        vector_memory_done();                                // (these are here before the loop: their loads are not waited for among the tiles')
         for (uint32_t step = 0; step < steps; ++step) {
             if (step + kAbStages - 1 < steps) {
                 tiles_landed<kLoads * (kAbStages - 2)>();
@@ -102,11 +100,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const f32x2* stats = ring_stats[now][wave_id()];
             if (row + kAbStep - 1 >= first) {                // (else none of these rows sees a key of this wave)
                 f32x16 s = {}, dp = {};
-#pragma unroll
-                for (int c = 0; c < kD / 16; ++c) {
-                    s = mma(read_along<T, kD>(ring[0][0], along, c), k[c], s);
-                    dp = mma(read_along<T, kD>(ring[0][0], along, c, kTile), v[c], dp);
-                }
+                products<kD / 8, 3, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
+                                       [&](int i, V8<T> r) {
+                                           if (i % 2 == 0) s = mma(r, k[i / 2], s);
+                                           else dp = mma(r, v[i / 2], dp);
+                                       });
                 const bool crosses = row < first + 31 || row + kAbStep > p.end;      // some of these rows do not see some of these keys, or are not the sequence's
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -121,14 +119,12 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                         if (r < key || r >= p.end) s[i] = dp[i] = 0.f;
                     }
                 // Weights and their gradients are rounded to T for the products; sums stay in 32 bits.
-                const V8<T> w0 = operand<T, 0>(s), w1 = operand<T, 1>(s), d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
-#pragma unroll
-                for (int d = 0; d < kD / 32; ++d) {
-                    dv[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile), w0, dv[d]);
-                    dv[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, kTile + 32 * kD), w1, dv[d]);
-                    dk[d] = mma(read_cross<T, kD>(ring[0][0], cross, d), d0, dk[d]);
-                    dk[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, 32 * kD), d1, dk[d]);
-                }
+                const V8<T> w[2] = {operand<T, 0>(s), operand<T, 1>(s)}, ds[2] = {operand<T, 0>(dp), operand<T, 1>(dp)};
+                products<kD / 8, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i / 4, i % 2 * kTile + i / 2 % 2 * 32 * kD); },
+                                       [&](int i, V8<T> r) {
+                                           if (i % 2 == 0) dk[i / 4] = mma(r, ds[i / 2 % 2], dk[i / 4]);
+                                           else dv[i / 4] = mma(r, w[i / 2 % 2], dv[i / 4]);
+                                       });
             }
             row += kAbStep;
             if (row >= p.end) row = p.first;
@@ -171,10 +167,6 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const uint32_t last = p.end - 1, kv = head / a.group, mine = umin(row, last);
         const T* k = a.k.at(0, kv);
         const T* v = a.v.at(0, kv);
-        V8<T> q[kD / 16], d_o[kD / 16];
-        load_row<T, kD, kFull>(q, a.q.at(mine, head), a.head_dim);
-        load_row<T, kD, kFull>(d_o, a.d_o.at(mine, head), a.head_dim);
-        const f32x2 stats = a.stats[(uint64_t)head * a.tokens + mine];
         const float scale = a.scale * kLog2e;
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
@@ -187,6 +179,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         };
         if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
         for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch(step);
+        V8<T> q[kD / 16], d_o[kD / 16];
+        load_row<T, kD, kFull>(q, a.q.at(mine, head), a.head_dim);
+        load_row<T, kD, kFull>(d_o, a.d_o.at(mine, head), a.head_dim);
+        const f32x2 stats = a.stats[(uint64_t)head * a.tokens + mine];
+        vector_memory_done();
         for (uint32_t step = 0; step < steps; ++step) {
             const uint32_t key = p.begin + step * kAbStep;
             if (step + kAbStages - 1 < steps) {
@@ -198,11 +195,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const uint32_t tile = step % kAbStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
             if (key > first + 31) continue;                  // (none of the wave's rows sees any of these keys)
             f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int c = 0; c < kD / 16; ++c) {
-                s = mma(read_along<T, kD>(ring[0][0], along, c), q[c], s);
-                dp = mma(read_along<T, kD>(ring[0][0], along, c, kTile), d_o[c], dp);
-            }
+            products<kD / 8, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
+                                   [&](int i, V8<T> r) {
+                                       if (i % 2 == 0) s = mma(r, q[i / 2], s);
+                                       else dp = mma(r, d_o[i / 2], dp);
+                                   });
             const bool crosses = key + 31 > first;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -213,12 +210,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (key + row_of(i, half) > row) dp[i] = 0.f;
-            const V8<T> d0 = operand<T, 0>(dp), d1 = operand<T, 1>(dp);
-#pragma unroll
-            for (int d = 0; d < kD / 32; ++d) {
-                dq[d] = mma(read_cross<T, kD>(ring[0][0], cross, d), d0, dq[d]);
-                dq[d] = mma(read_cross<T, kD>(ring[0][0], cross, d, 32 * kD), d1, dq[d]);
-            }
+            const V8<T> ds[2] = {operand<T, 0>(dp), operand<T, 1>(dp)};
+            constexpr int kDs = kD / 32;
+            products<2 * kDs, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
+                                    [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
     }
     if (row < p.end) store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);

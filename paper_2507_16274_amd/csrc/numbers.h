@@ -43,6 +43,17 @@ template <typename T> __device__ __forceinline__ f32x8 load_some(const T* p, int
     for (int i = 0; i < 8; ++i) x[i] = i < n ? (float)p[i] : fill;
     return x;
 }
+// The same, left in the type it has in memory; zeros in place of the others.
+template <typename T> __device__ __forceinline__ typename Vec<T>::x8 packed_some(const T* p, int n)
+{
+    typename Vec<T>::x8 v = {};
+    if (n >= 8) __builtin_memcpy(&v, p, sizeof(v));
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) v[i] = p[i];
+    return v;
+}
 template <typename T> __device__ __forceinline__ void store_some(T* p, int n, f32x8 x)
 {
     if (n >= 8) { store8(p, x); return; }

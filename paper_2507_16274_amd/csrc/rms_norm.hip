@@ -3,9 +3,9 @@
 //     s = round(x + r),   rstd = 1 / sqrt(mean(s^2) + eps),   y = s rstd w,
 //     dx = rstd (g - s rstd^2 mean(g s)) + ds   with g = w dy,   dw = sum over rows of dy s rstd.
 //
-// Both are bound by device memory: a handful of operations per number.  A team of 64, 256 or 1024 threads keeps a whole
-// row in registers between its two looks at it (the sum, then the scaled output), so every input is read once and every
-// output written once.  Eight neighbouring numbers belong to a thread: 16-byte accesses, and 128 columns -- what
+// Both are bound by device memory: a handful of operations per number.  A team of threads, a wave for up to 1024 columns and a workgroup of as many waves as
+// the row needs beyond, keeps a whole row in registers between its two looks at it (the sum, then the scaled output), so every input is
+// read once and every output written once.  Eight neighbouring numbers belong to a thread: 16-byte accesses, and 128 columns -- what
 // one 8-bit scale covers -- are one DPP row of 16 lanes.
 #include "numbers.h"
 
@@ -29,17 +29,15 @@ struct NormArgs {
     float* rstd;
 };
 
-// Sum over the kTeam threads of a team (whole waves), in all of them.  `part`: one word per wave, not in use.
-template <int kTeam> __device__ __forceinline__ float team_sum(float v, float* part)
+// Sum over a team, in all of its threads: a wave (kWaveTeam) or the workgroup.  `part`: one word per wave, not in use.
+template <bool kWaveTeam> __device__ __forceinline__ float team_sum(float v, float* part)
 {
     v = wave_sum(v);
-    if (kTeam == kWave) return v;
-    constexpr int kWaves = kTeam / kWave;
+    if (kWaveTeam) return v;
     if (lane_id() == 0) part[wave_id()] = v;
     __syncthreads();
     float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) total += part[i];      // (256 and 1024 threads are a workgroup: one team)
+    for (uint32_t i = 0; i < blockDim.x / kWave; ++i) total += part[i];
     return total;
 }
 
@@ -97,27 +95,26 @@ template <typename T> __device__ __forceinline__ void emit(const NormArgs& a, ui
     if (a.q) store_eight_bits(y, row, a.width, col, a.q, a.scales);
 }
 
-// One team per row, kGroups groups of 8 numbers per thread: width <= 8 * kTeam * kGroups.
-template <typename T, int kTeam, int kGroups>
-__global__ void __launch_bounds__(kTeam < 256 ? 256 : kTeam) norm_rows(NormArgs a)
+// One team per row, kGroups groups of 8 numbers per thread.
+template <typename T, bool kWaveTeam, int kGroups> __global__ void __launch_bounds__(kWaveTeam ? 256 : 1024) norm_rows(NormArgs a)
 {
-    __shared__ float part[kTeam / kWave];
-    constexpr int kTeams = kTeam < 256 ? 256 / kTeam : 1;
-    const uint32_t row = blockIdx.x * kTeams + threadIdx.x / kTeam, t = threadIdx.x % kTeam;
-    if (row >= a.rows) return;                               // (a whole wave; teams of more than one wave have one row a workgroup)
+    __shared__ float part[1024 / kWave];
+    const uint32_t team = kWaveTeam ? kWave : blockDim.x;
+    const uint32_t row = kWaveTeam ? blockIdx.x * 4 + wave_id() : blockIdx.x, t = kWaveTeam ? lane_id() : threadIdx.x;
+    if (row >= a.rows) return;                               // (a whole wave; a workgroup that is a team has a row)
     f32x8 s[kGroups];
     float total = 0.f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        const uint32_t col = (g * kTeam + t) * 8;
+        const uint32_t col = (g * team + t) * 8;
         s[g] = f32x8{};
         if (col < a.width) s[g] = add_and_keep<T>(a, row, col);
         total += square(s[g]);
     }
-    const float rstd = 1.f / sqrtf(team_sum<kTeam>(total, part) / (float)a.width + a.eps);
+    const float rstd = 1.f / sqrtf(team_sum<kWaveTeam>(total, part) / (float)a.width + a.eps);
     if (t == 0) a.rstd[row] = rstd;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) emit<T>(a, row, (g * kTeam + t) * 8, s[g], rstd);
+    for (int g = 0; g < kGroups; ++g) emit<T>(a, row, (g * team + t) * 8, s[g], rstd);
 }
 
 // Rows too wide for registers: the second look is at what the first one kept (or at x, where there is no residual).
@@ -127,7 +124,7 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_wide(NormArgs
     const uint32_t row = blockIdx.x;
     float total = 0.f;
     for (uint64_t col = threadIdx.x * 8; col < a.width; col += 8192) total += square(add_and_keep<T>(a, row, (uint32_t)col));
-    const float rstd = 1.f / sqrtf(team_sum<1024>(total, part) / (float)a.width + a.eps);
+    const float rstd = 1.f / sqrtf(team_sum<false>(total, part) / (float)a.width + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
     const T* kept = a.sum ? (const T*)a.sum + (uint64_t)row * a.width : (const T*)a.x + row * a.x_stride;
     for (uint64_t base = 0; base < a.width; base += 8192) {  // (all lanes stay: 128 columns are reduced over 16 of them)
@@ -159,56 +156,72 @@ __device__ __forceinline__ float dot(f32x8 a, f32x8 b)
     return v;
 }
 
-template <typename T> __device__ __forceinline__ void emit_dx(const NormBackwardArgs& a, uint32_t row, uint32_t col, f32x8 g, f32x8 s, float r, float c)
+template <typename T> __device__ __forceinline__ void emit_dx(const NormBackwardArgs& a, uint32_t row, uint32_t col, f32x8 g, f32x8 s, f32x8 d_sum, float r, float c)
 {
-    const int n = (int)(a.width - col);
-    f32x8 d = r * (g - s * (r * r * c));
-    const uint64_t at = (uint64_t)row * a.width + col;
-    if (a.d_sum) d += load_some((const T*)a.d_sum + at, n, 0.f);
-    store_some((T*)a.dx + at, n, d);
+    store_some((T*)a.dx + (uint64_t)row * a.width + col, (int)(a.width - col), r * (g - s * (r * r * c)) + d_sum);
 }
 
-// Every team walks over rows of its own; the thread's columns stay the same, so the weight and the sums of dw are in registers.
-template <typename T, int kTeam, int kGroups>
-__global__ void __launch_bounds__(kTeam < 256 ? 256 : kTeam) norm_backward_rows(NormBackwardArgs a)
+// Every team walks over rows of its own; the thread's columns stay the same, so the weight and the sums of dw are in registers.  The next row is on its way,
+// in the type it has in memory, while this one's sum goes round: two teams a CU are enough then, and leave half the
+// sums to add up that four would (8192 rows of 5120: 138 us without that and 768 teams, 66 with it).
+// kAhead: whether there are registers for that (not with 1024 threads).
+template <typename T, bool kWaveTeam, int kGroups, int kThreads, bool kAhead> __global__ void __launch_bounds__(kThreads) norm_backward_rows(NormBackwardArgs a)
 {
-    __shared__ float part[2][kTeam / kWave];
-    constexpr int kTeams = kTeam < 256 ? 256 / kTeam : 1;
-    const uint32_t team = blockIdx.x * kTeams + threadIdx.x / kTeam, t = threadIdx.x % kTeam, teams = gridDim.x * kTeams;
+    __shared__ float part[2][1024 / kWave];
+    using Packed = typename Vec<T>::x8;
+    const uint32_t size = kWaveTeam ? kWave : blockDim.x, t = kWaveTeam ? lane_id() : threadIdx.x;
+    const uint32_t team = kWaveTeam ? blockIdx.x * 4 + wave_id() : blockIdx.x, teams = kWaveTeam ? gridDim.x * 4 : gridDim.x;
+    const auto wide = [](Packed v) { return __builtin_convertvector(v, f32x8); };
     f32x8 w[kGroups], dw[kGroups];
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        const uint32_t col = (g * kTeam + t) * 8;
+        const uint32_t col = (g * size + t) * 8;
         dw[g] = w[g] = f32x8{};
         if (col < a.width) w[g] = load_some((const T*)a.weight + col, (int)(a.width - col), 0.f);
     }
+    Packed dy[kGroups], s[kGroups], ds[kGroups];
+    float r = 0.f;
+    const auto fetch = [&](uint32_t row) {
+        r = a.rstd[row];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const uint32_t col = (g * size + t) * 8;
+            const int n = (int)a.width - (int)col;
+            const uint64_t at = (uint64_t)row * a.width + col;
+            dy[g] = s[g] = ds[g] = Packed{};
+            if (n <= 0) continue;
+            dy[g] = packed_some((const T*)a.d_y + row * a.d_y_stride + col, n);
+            s[g] = packed_some((const T*)a.sum + at, n);
+            if (a.d_sum) ds[g] = packed_some((const T*)a.d_sum + at, n);
+        }
+    };
+    if (kAhead && team < a.rows) fetch(team);
     uint32_t turn = 0;
     for (uint32_t row = team; row < a.rows; row += teams, turn ^= 1) {
-        f32x8 dy[kGroups], s[kGroups];
+        if (!kAhead) fetch(row);
+        Packed dy_now[kGroups], s_now[kGroups], ds_now[kGroups];
+        const float r_now = r;
         float total = 0.f;
-        const float r = a.rstd[row];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const uint32_t col = (g * kTeam + t) * 8;
-            dy[g] = s[g] = f32x8{};
-            if (col < a.width) {
-                const int n = (int)(a.width - col);
-                dy[g] = load_some((const T*)a.d_y + row * a.d_y_stride + col, n, 0.f);
-                s[g] = load_some((const T*)a.sum + (uint64_t)row * a.width + col, n, 0.f);
-            }
-            total += dot(dy[g] * w[g], s[g]);
+            dy_now[g] = dy[g];
+            s_now[g] = s[g];
+            ds_now[g] = ds[g];
+            total += dot(wide(dy[g]) * w[g], wide(s[g]));
         }
-        const float c = team_sum<kTeam>(total, part[turn]) / (float)a.width;   // (two words in turn: one barrier a row)
+        if (kAhead && row + teams < a.rows) fetch(row + teams);        // (dx may lie in place of d_y or d_sum: in this row's, never in the next one's)
+        const float c = team_sum<kWaveTeam>(total, part[turn]) / (float)a.width;   // (two words in turn: one barrier a row)
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const uint32_t col = (g * kTeam + t) * 8;
-            dw[g] += dy[g] * s[g] * r;
-            if (col < a.width) emit_dx<T>(a, row, col, dy[g] * w[g], s[g], r, c);
+            const uint32_t col = (g * size + t) * 8;
+            const f32x8 y = wide(dy_now[g]), x = wide(s_now[g]);
+            dw[g] += y * x * r_now;
+            if (col < a.width) emit_dx<T>(a, row, col, y * w[g], x, wide(ds_now[g]), r_now, c);
         }
     }
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        const uint32_t col = (g * kTeam + t) * 8;
+        const uint32_t col = (g * size + t) * 8;
         if (col < a.width) store_some(a.part + (uint64_t)team * a.width + col, (int)(a.width - col), dw[g]);
     }
 }
@@ -226,10 +239,12 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_backward_wide
         const int n = (int)(a.width - col);
         total += dot(load_some(dy + col, n, 0.f) * load_some(w + col, n, 0.f), load_some(s + col, n, 0.f));
     }
-    const float c = team_sum<1024>(total, part) / (float)a.width;
+    const float c = team_sum<false>(total, part) / (float)a.width;
     for (uint64_t col = threadIdx.x * 8; col < a.width; col += 8192) {
         const int n = (int)(a.width - col);
-        emit_dx<T>(a, row, (uint32_t)col, load_some(dy + col, n, 0.f) * load_some(w + col, n, 0.f), load_some(s + col, n, 0.f), r, c);
+        f32x8 through = {};
+        if (a.d_sum) through = load_some((const T*)a.d_sum + (uint64_t)row * a.width + col, n, 0.f);
+        emit_dx<T>(a, row, (uint32_t)col, load_some(dy + col, n, 0.f) * load_some(w + col, n, 0.f), load_some(s + col, n, 0.f), through, r, c);
     }
 }
 
@@ -245,33 +260,45 @@ template <typename T> __global__ void __launch_bounds__(256) norm_dweight_wide(N
     store_some(a.part + (uint64_t)blockIdx.y * a.width + col, n, dw);
 }
 
-// dweight[c] = sum over the teams, in their order: 64 columns a workgroup, four waves that take a quarter of the teams each.
-__global__ void __launch_bounds__(256) norm_dweight(const float* __restrict__ part, uint32_t teams, uint32_t width, float* dweight)
+// dweight[c] = sum over the teams, in a fixed order: 64 columns a workgroup, sixteen waves that take a share of the teams each.
+__global__ void __launch_bounds__(1024) norm_dweight(const float* __restrict__ part, uint32_t teams, uint32_t width, float* dweight)
 {
-    __shared__ float sums[4][kWave];
+    __shared__ float sums[16][kWave];
     const uint32_t col = blockIdx.x * kWave + lane_id(), w = wave_id();
     float total = 0.f;
     if (col < width) {
-        const uint32_t from = (uint32_t)((uint64_t)teams * w / 4), to = (uint32_t)((uint64_t)teams * (w + 1) / 4);
+        const uint32_t from = (uint32_t)((uint64_t)teams * w / 16), to = (uint32_t)((uint64_t)teams * (w + 1) / 16);
 #pragma unroll 8
         for (uint32_t i = from; i < to; ++i) total += part[(uint64_t)i * width + col];
     }
     sums[w][lane_id()] = total;
     __syncthreads();
-    if (w == 0 && col < width) dweight[col] = (sums[0][lane_id()] + sums[1][lane_id()]) + (sums[2][lane_id()] + sums[3][lane_id()]);
+    if (w != 0 || col >= width) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) total += sums[i][lane_id()];
+    dweight[col] = total;
 }
 
-constexpr uint32_t kWidest = 8 * 1024 * 4;                   // what a team of 1024 threads keeps in registers
+constexpr uint32_t kWaveWidth = 1024;                        // rows up to here are a wave's
+constexpr uint32_t kWidest = 8 * 1024 * 4, kWidestBackward = 8 * 1024 * 2;         // what a team of 1024 threads keeps in registers
 
-inline uint32_t team_of(uint32_t width) { return width <= 1024 ? 64 : width <= 8192 ? 256 : 1024; }
+// How a row is shared out: groups of 8 numbers a thread (two, four where two would take more than 1024 threads), and the threads of a workgroup.
+struct NormShape {
+    uint32_t groups, threads;
+};
+inline NormShape norm_shape(uint32_t width)
+{
+    if (width <= kWaveWidth) return {width <= 512 ? 1u : 2u, 256};
+    const uint32_t groups = width <= 16384 ? 2 : 4, threads = (width + 8 * groups - 1) / (8 * groups);
+    return {groups, (threads + kWave - 1) / kWave * kWave};
+}
 
-// Teams of the backward kernel, each with a row of partial sums: enough for the waves that fill the chip.
+// Teams of the backward kernel, each with a row of partial sums: eight waves a CU as teams of one wave, else two teams a CU.
 inline uint32_t teams_of(uint32_t rows, uint32_t width)
 {
-    if (width > kWidest) return umin_host(rows, 64);
-    const uint32_t team = team_of(width), most = team == 64 ? 2048 : team == 256 ? 768 : 256;
-    const uint32_t teams = umin_host(rows, most);
-    return team == 64 ? (teams + 3) / 4 * 4 : teams;
+    if (width > kWidestBackward) return umin_host(rows, 64);
+    if (width <= kWaveWidth) return (umin_host(rows, 2048) + 3) / 4 * 4;
+    return umin_host(rows, 512);
 }
 
 }  // namespace stalloc
@@ -282,32 +309,26 @@ namespace {
 
 template <typename T> void launch_norm(const NormArgs& a, hipStream_t stream)
 {
-    const uint32_t groups = (uint32_t)(((uint64_t)a.width + 8 * team_of(a.width) - 1) / (8 * team_of(a.width)));
+    const NormShape shape = norm_shape(a.width);
     const auto one = [&](auto kernel, uint32_t blocks, uint32_t threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a); };
     if (a.width > kWidest) one(norm_wide<T>, a.rows, 1024);
-    else if (team_of(a.width) == 64 && groups == 1) one(norm_rows<T, 64, 1>, (a.rows - 1) / 4 + 1, 256);
-    else if (team_of(a.width) == 64) one(norm_rows<T, 64, 2>, (a.rows - 1) / 4 + 1, 256);
-    else if (team_of(a.width) == 256 && groups == 1) one(norm_rows<T, 256, 1>, a.rows, 256);
-    else if (team_of(a.width) == 256 && groups == 2) one(norm_rows<T, 256, 2>, a.rows, 256);
-    else if (team_of(a.width) == 256) one(norm_rows<T, 256, 4>, a.rows, 256);
-    else if (groups <= 2) one(norm_rows<T, 1024, 2>, a.rows, 1024);
-    else one(norm_rows<T, 1024, 4>, a.rows, 1024);
+    else if (a.width <= kWaveWidth && shape.groups == 1) one(norm_rows<T, true, 1>, (a.rows - 1) / 4 + 1, 256);
+    else if (a.width <= kWaveWidth) one(norm_rows<T, true, 2>, (a.rows - 1) / 4 + 1, 256);
+    else if (shape.groups == 2) one(norm_rows<T, false, 2>, a.rows, shape.threads);
+    else one(norm_rows<T, false, 4>, a.rows, shape.threads);
 }
 
 template <typename T> void launch_norm_backward(const NormBackwardArgs& a, uint32_t teams, hipStream_t stream)
 {
-    const uint32_t groups = (uint32_t)(((uint64_t)a.width + 8 * team_of(a.width) - 1) / (8 * team_of(a.width)));
+    const NormShape shape = norm_shape(a.width);
     const auto one = [&](auto kernel, uint32_t blocks, uint32_t threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a); };
-    if (a.width > kWidest) {
+    if (a.width > kWidestBackward) {
         hipLaunchKernelGGL(norm_dweight_wide<T>, dim3((a.width + 2047) / 2048, teams), dim3(256), 0, stream, a);
         one(norm_backward_wide<T>, a.rows, 1024);
-    } else if (team_of(a.width) == 64 && groups == 1) one(norm_backward_rows<T, 64, 1>, teams / 4, 256);
-    else if (team_of(a.width) == 64) one(norm_backward_rows<T, 64, 2>, teams / 4, 256);
-    else if (team_of(a.width) == 256 && groups == 1) one(norm_backward_rows<T, 256, 1>, teams, 256);
-    else if (team_of(a.width) == 256 && groups == 2) one(norm_backward_rows<T, 256, 2>, teams, 256);
-    else if (team_of(a.width) == 256) one(norm_backward_rows<T, 256, 4>, teams, 256);
-    else if (groups <= 2) one(norm_backward_rows<T, 1024, 2>, teams, 1024);
-    else one(norm_backward_rows<T, 1024, 4>, teams, 1024);
+    } else if (a.width <= kWaveWidth && shape.groups == 1) one(norm_backward_rows<T, true, 1, 256, true>, teams / 4, 256);
+    else if (a.width <= kWaveWidth) one(norm_backward_rows<T, true, 2, 256, true>, teams / 4, 256);
+    else if (shape.threads <= 512) one(norm_backward_rows<T, false, 2, 512, true>, teams, shape.threads);
+    else one(norm_backward_rows<T, false, 2, 1024, false>, teams, shape.threads);
 }
 
 bool norm_sizes_ok(uint32_t dtype, uint32_t rows, uint32_t width)
@@ -345,6 +366,6 @@ extern "C" int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t
     const NormBackwardArgs a = {rows, width, d_y, d_y_stride, sum, weight, rstd, d_sum, dx, part};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     with_type(dtype, [&](auto t) { launch_norm_backward<decltype(t)>(a, teams, stream); });
-    hipLaunchKernelGGL(norm_dweight, dim3((width + kWave - 1) / kWave), dim3(256), 0, stream, part, teams, width, dweight);
+    hipLaunchKernelGGL(norm_dweight, dim3((width + kWave - 1) / kWave), dim3(1024), 0, stream, part, teams, width, dweight);
     return launched();
 }

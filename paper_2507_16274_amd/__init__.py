@@ -133,7 +133,9 @@ def _trace(size: torch.Tensor, t_alloc: torch.Tensor, t_free: torch.Tensor, t_en
 
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-    return (stream or torch.cuda.current_stream()).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())      # (current_stream() makes an object first: 2.7 us)
 
 
 def _workspace(nbytes: int, device, cache: Optional[Dict]) -> torch.Tensor:
@@ -445,7 +447,12 @@ def _flat(t: Optional[torch.Tensor], name: str) -> Optional[int]:
 
 
 def _call(fn, name, args, like, stream, workspace_cache, out):
-    """Query, workspace, call."""
+    """Query, workspace, call.  With a workspace at hand the call comes first: it takes one that is large enough."""
+    ws = workspace_cache.get("ws") if workspace_cache is not None else None
+    if ws is not None:
+        if fn(*args, ws.data_ptr(), ctypes.byref(ctypes.c_size_t(ws.numel())), _stream(stream)) == 0:
+            out["workspace"] = ws
+            return out
     need = ctypes.c_size_t(0)
     _check(fn(*args, None, ctypes.byref(need), None), name + "(workspace query)")
     if stream is None:

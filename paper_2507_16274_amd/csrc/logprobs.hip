@@ -8,8 +8,9 @@
 // into parts so that the whole chip reads, and a wave per row joins them.
 //
 // The most likely tokens cost no second pass: a thread remembers which group of eight gave it its maximum (the running maximum
-// it needs anyway).  The largest of the workgroup's 256 maxima is the row's first; the thread that owned it then offers its next best,
-// for which its numbers alone (a 256th of the row) are looked at again.
+// it needs anyway).  The k-th largest of the 256 maxima bounds the k-th largest number from below, and the numbers that reach it all belong to the
+// k threads with the largest maxima: those threads' numbers alone (k 256ths of the part) are looked at again, by whole waves, and what
+// reaches the bound, hardly more than k numbers as a rule, is put in order by counting.
 #include <math.h>
 
 #include "numbers.h"
@@ -61,13 +62,20 @@ __device__ __forceinline__ void join(Softmax& s, Softmax o)
     s.a += o.a;
 }
 
-__device__ __forceinline__ Softmax from_lane_xor(const Softmax& s, int step)
+// Over the lanes of a wave, in all of them: to one maximum first, then sums.
+__device__ __forceinline__ Softmax join_wave(Softmax s)
 {
-    Softmax o;
-    o.m = __shfl_xor(s.m, step, kWave);
-    o.z = __shfl_xor(s.z, step, kWave);
-    o.a = __shfl_xor(s.a, step, kWave);
-    return o;
+    float m = s.m;
+    m = fmaxf(m, dpp<kDppRowRor8>(kLowest, m));
+    m = fmaxf(m, dpp<kDppRowRor4>(kLowest, m));
+    m = fmaxf(m, dpp<kDppRowRor2>(kLowest, m));
+    m = fmaxf(m, dpp<kDppRowRor1>(kLowest, m));
+    m = fmaxf(m, dpp<kDppRowBcast15, 0xa>(kLowest, m));
+    m = fmaxf(m, dpp<kDppRowBcast31, 0xc>(kLowest, m));
+    rebase(s, as_float(__builtin_amdgcn_readlane(as_bits(m), kWave - 1)));
+    s.z = wave_sum(s.z);
+    s.a = wave_sum(s.a);
+    return s;
 }
 
 __device__ __forceinline__ Softmax with_eight(Softmax s, f32x8 v)
@@ -86,8 +94,7 @@ __device__ __forceinline__ Softmax with_eight(Softmax s, f32x8 v)
 // Over the workgroup's threads, in all of them and in one order.
 __device__ __forceinline__ Softmax join_workgroup(Softmax s, Softmax* waves)
 {
-#pragma unroll
-    for (int step = 1; step < kWave; step <<= 1) join(s, from_lane_xor(s, step));
+    s = join_wave(s);
     if (lane_id() == 0) waves[wave_id()] = s;
     __syncthreads();
     s = waves[0];
@@ -111,13 +118,23 @@ struct LogprobArgs {
     uint64_t* keys;                                          // [rows][parts][top]
 };
 
-template <typename T> __device__ __forceinline__ void finish_row(const LogprobArgs& a, uint32_t row, const Softmax& s)
+// The row's token and its logit: asked for when a workgroup begins, wanted when it ends.
+struct Target {
+    int32_t token;
+    float logit;
+};
+template <typename T> __device__ __forceinline__ Target target_of(const LogprobArgs& a, uint32_t row)
+{
+    Target t = {a.tokens[row], 0.f};
+    if (t.token >= (int32_t)a.vocabulary) t.token = -1;
+    if (t.token >= 0) t.logit = (float)((const T*)a.logits)[row * a.row_stride + t.token];
+    return t;
+}
+
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, uint32_t row, const Softmax& s, Target target)
 {
     const float ln_z = logf(s.z);                            // (log 0 = -infinity: nothing can occur)
-    const int32_t token = a.tokens[row];
-    float lp = 0.f;
-    if (token >= 0 && token < (int32_t)a.vocabulary) lp = s.z == 0.f ? -INFINITY : ((float)((const T*)a.logits)[row * a.row_stride + token] - s.m) - ln_z;
-    a.logprob[row] = lp;
+    a.logprob[row] = target.token < 0 ? 0.f : s.z == 0.f ? -INFINITY : (target.logit - s.m) - ln_z;
     a.entropy[row] = s.z == 0.f ? 0.f : ln_z - s.a / s.z * kLn2;
     a.lse[row] = s.z == 0.f ? -INFINITY : s.m + ln_z;
 }
@@ -141,16 +158,28 @@ __device__ __forceinline__ void check_tokens(const int32_t* __restrict__ tokens,
     if (threadIdx.x == 0) *status = words[0] | words[1] | words[2] | words[3] ? STALLOC_ERR_BAD_TOKEN : STALLOC_OK;
 }
 
+// The key of rank `rank` of the workgroup's part: to the row's outputs, or to the part's list.
+__device__ __forceinline__ void put_key(const LogprobArgs& a, uint32_t row, uint32_t rank, uint64_t key, const Softmax& s)
+{
+    if (a.parts > 1) a.keys[(uint64_t)blockIdx.x * a.top + rank] = key;
+    else put_top(a, row, rank, key, s);
+}
+
+constexpr uint32_t kMostFound = 1024;
+
 // A workgroup takes one part of one row.
 template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_row(LogprobArgs a)
 {
     __shared__ Softmax waves[kLpThreads / kWave];
-    __shared__ uint64_t best[kLpThreads];
+    __shared__ uint64_t best[kLpThreads], rows_best[kLpThreads / 16], list[kMostFound], bound;
+    __shared__ uint32_t found[2];
+    __shared__ uint8_t first[kLpThreads];
     __shared__ uint32_t words[kLpThreads / kWave];
     if (blockIdx.x == 0) check_tokens(a.tokens, a.rows, a.vocabulary, a.status, words);
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts, t = threadIdx.x;
     const T* x = (const T*)a.logits + row * a.row_stride;
     const uint32_t from = part * a.part_width, to = umin(a.vocabulary, from + a.part_width);   // (the last parts may be empty: from >= to)
+    const Target target = target_of<T>(a, row);
     Softmax s = of_nothing();
     float most = -INFINITY;                                  // this thread's maximum, and where it was met first
     uint32_t group = from + t * 8;
@@ -171,60 +200,130 @@ template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_row(Logpr
         }
         best[t] = k;
     }
-    s = join_workgroup(s, waves);
-    if (wave_id() != 0) return;
-    if (a.parts > 1) {
-        if (t == 0) a.part[blockIdx.x] = s;
-    } else if (t == 0) {
-        finish_row<T>(a, row, s);
+    s = join_workgroup(s, waves);                            // (behind its barrier the maxima are there as well)
+    if (t == 0) {
+        if (a.parts > 1) a.part[blockIdx.x] = s;
+        else finish_row(a, row, s, target);
     }
-    uint64_t mine[kLpThreads / kWave];                       // lane l looks after the threads 4 l .. 4 l + 3
+    if (!a.top) return;
+
+    // Ranks among the maxima (all different but for threads without numbers, which have 0): the first `top` threads, and their last one's maximum.  For up to
+    // 16 only maxima that reach the `top`-th largest of the 16 DPP rows' take part.
+    const uint32_t top = a.top, threads = (to > from ? to - from + 7 : 0) / 8;       // threads with numbers
+    const uint64_t mine = best[t];
+    uint64_t row_best = mine;
+    row_best = umax64(row_best, dpp64<kDppRowRor1>(0, row_best));
+    row_best = umax64(row_best, dpp64<kDppRowRor2>(0, row_best));
+    row_best = umax64(row_best, dpp64<kDppRowRor4>(0, row_best));
+    row_best = umax64(row_best, dpp64<kDppRowRor8>(0, row_best));
+    if ((t & 15) == 0) rows_best[t / 16] = row_best;
+    if (t < 2) found[t] = 0;
+    if (t == 0) bound = 1;                                   // (fewer than `top` maxima: all numbers count)
+    __syncthreads();
+    uint64_t pivot = 1;
+    if (top <= kLpThreads / 16) {
+        const uint64_t other = rows_best[t & 15];
+        uint32_t larger = 0;
 #pragma unroll
-    for (int i = 0; i < kLpThreads / kWave; ++i) mine[i] = a.top ? best[t * (kLpThreads / kWave) + i] : 0;
-    for (uint32_t rank = 0; rank < a.top; ++rank) {
-        uint64_t k = mine[0];
-#pragma unroll
-        for (int i = 1; i < kLpThreads / kWave; ++i) k = umax64(k, mine[i]);
-        k = wave_max64(k);
-        if (a.parts > 1) { if (t == 0) a.keys[(uint64_t)blockIdx.x * a.top + rank] = k; }
-        else if (t == 0) put_top(a, row, rank, k, s);
-        if (rank + 1 == a.top) break;
-        const uint32_t owner = ((place_of(k) - from) / 8) % kLpThreads;
-        uint64_t next = 0;                                   // the owner's largest key below the one taken
-        for (uint32_t at = from + (owner + t * kLpThreads) * 8; at < to; at += kWave * kLpThreads * 8) {
+        for (int i = 0; i < kLpThreads / 16; ++i) larger += rows_best[i] > other;
+        const uint64_t at = __ballot(larger == top - 1 && other != 0);
+        if (at) pivot = readlane64(other, __builtin_ctzll(at));
+    }
+    if (mine >= pivot) list[atomicAdd(&found[0], 1u)] = mine;
+    __syncthreads();
+    if (t < found[0]) {
+        const uint64_t k = list[t];
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (uint32_t i = 0; i < found[0]; ++i) rank += list[i] > k;
+        if (rank < top) first[rank] = (uint8_t)((place_of(k) - from) / 8 % kLpThreads);
+        if (rank == top - 1) bound = k;
+    }
+    __syncthreads();
+    const uint64_t least = bound;
+    for (uint32_t i = wave_id(); i < umin(top, threads); i += kLpThreads / kWave)
+        for (uint32_t at = from + (first[i] + lane_id() * kLpThreads) * 8; at < to; at += kWave * kLpThreads * 8) {
             const f32x8 v = load_some(x + at, (int)(to - at), -INFINITY);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint64_t other = key_of(v[i], at + i);
-                if (at + i < to && other < k) next = umax64(next, other);
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t k = key_of(v[j], at + j);
+                if (at + j >= to || k < least) continue;
+                const uint32_t place = atomicAdd(&found[1], 1u);
+                if (place < kMostFound) list[place] = k;
             }
         }
-        next = wave_max64(next);
-        if (t == owner / (kLpThreads / kWave)) {
-#pragma unroll
-            for (int i = 0; i < kLpThreads / kWave; ++i)
-                if (owner % (kLpThreads / kWave) == (uint32_t)i) mine[i] = next;
+    __syncthreads();
+    const uint32_t n = found[1];
+    if (n <= kMostFound) {
+        for (uint32_t i = t; i < n; i += kLpThreads) {
+            const uint64_t k = list[i];
+            uint32_t r = 0;
+#pragma unroll 4
+            for (uint32_t j = 0; j < n; ++j) r += list[j] > k;
+            if (r < top) put_key(a, row, r, k, s);
         }
+        for (uint32_t i = n + t; i < top; i += kLpThreads) put_key(a, row, i, 0, s);       // (a part shorter than `top`)
+        return;
+    }
+    // More than there is room for (thousands of large numbers in few threads' columns): one after the other, each the largest below the one before.
+    uint64_t below = ~0ull;
+    for (uint32_t r = 0; r < top; ++r) {
+        uint64_t k = 0;
+        for (uint32_t at = from + t * 8; at < to; at += kLpThreads * 8) {
+            const f32x8 v = load_some(x + at, (int)(to - at), -INFINITY);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t other = key_of(v[j], at + j);
+                if (at + j < to && other < below) k = umax64(k, other);
+            }
+        }
+        k = wave_max64(k);
+        __syncthreads();
+        if (lane_id() == 0) best[wave_id()] = k;
+        __syncthreads();
+        for (int i = 0; i < kLpThreads / kWave; ++i) k = umax64(k, best[i]);
+        if (t == 0) put_key(a, row, r, k, s);
+        below = k;
     }
 }
 
-// A wave joins the parts of a row (at most 64, a lane each) and picks the row's most likely tokens from theirs, which every part lists
-// in descending order: a lane holds the first one not taken yet.
-template <typename T> __global__ void __launch_bounds__(kWave) lp_join(LogprobArgs a)
+
+// A workgroup joins the parts of a row (at most 64), and picks the row's most likely tokens from theirs, which every part lists in descending
+// order: a key's rank is the number of larger keys, counted, or (more than 1024 of them) its place in its own list and, in each other one, the number of
+// larger keys, found by halving.
+template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_join(LogprobArgs a)
 {
-    const uint32_t row = blockIdx.x, lane = lane_id();
+    __shared__ uint64_t keys[kMostParts * kMostTop];
+    const uint32_t row = blockIdx.x, lane = lane_id(), all = a.parts * a.top;
+    for (uint32_t i = threadIdx.x; i < all; i += kLpThreads) keys[i] = a.keys[(uint64_t)row * all + i];
+    const Target target = target_of<T>(a, row);
     Softmax s = of_nothing();
     if (lane < a.parts) s = a.part[(uint64_t)row * a.parts + lane];
-#pragma unroll
-    for (int step = 1; step < kWave; step <<= 1) join(s, from_lane_xor(s, step));
-    if (lane == 0) finish_row<T>(a, row, s);
-    const uint64_t* list = a.keys + ((uint64_t)row * a.parts + lane) * a.top;
-    uint32_t taken = 0;
-    uint64_t k = lane < a.parts && a.top ? list[0] : 0;
-    for (uint32_t rank = 0; rank < a.top; ++rank) {
-        const uint64_t first = wave_max64(k);
-        if (lane == 0) put_top(a, row, rank, first, s);
-        if (lane < a.parts && k == first) k = ++taken < a.top ? list[taken] : 0;
+    s = join_wave(s);
+    if (threadIdx.x == 0) finish_row(a, row, s, target);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < all; i += kLpThreads) {
+        const uint64_t k = keys[i];
+        uint32_t rank = 0;
+        if (all <= 1024) {
+#pragma unroll 8
+            for (uint32_t j = 0; j < all; ++j) rank += keys[j] > k;
+        } else {
+            const uint32_t part = i / a.top;
+            rank = i % a.top;
+            for (uint32_t p = 0; p < a.parts && rank < a.top; ++p) {
+                if (p == part) continue;
+                const uint64_t* list = keys + p * a.top;
+                uint32_t lo = 0, hi = a.top;                 // list[0 .. lo) are larger, list[hi ..) are not
+                while (lo < hi) {
+                    const uint32_t mid = (lo + hi) / 2;
+                    if (list[mid] > k) lo = mid + 1;
+                    else hi = mid;
+                }
+                rank += lo;
+            }
+        }
+        if (k && rank < a.top) put_top(a, row, rank, k, s);
     }
 }
 
@@ -254,7 +353,7 @@ template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_backward(
     __shared__ uint32_t words[kLpThreads / kWave];
     __shared__ Softmax waves[kLpThreads / kWave];
     if (blockIdx.x == 0) check_tokens(a.tokens, a.rows, a.vocabulary, a.status, words);
-    const uint32_t row = blockIdx.x / a.chunks;
+    const uint32_t row = a.rows - 1 - blockIdx.x / a.chunks;  // last rows first: they are what the forward pass left in the caches
     uint32_t chunk = blockIdx.x % a.chunks, end = chunk + 1;
     const T* x = (const T*)a.logits + row * a.row_stride;
     T* d = (T*)a.d_logits + row * a.d_row_stride;
@@ -338,7 +437,7 @@ extern "C" int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vo
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL(lp_row<T>, dim3(rows * shape.parts), dim3(kLpThreads), 0, stream, a);
-        if (shape.parts > 1) hipLaunchKernelGGL(lp_join<T>, dim3(rows), dim3(kWave), 0, stream, a);
+        if (shape.parts > 1) hipLaunchKernelGGL(lp_join<T>, dim3(rows), dim3(kLpThreads), 0, stream, a);
     });
     return launched();
 }

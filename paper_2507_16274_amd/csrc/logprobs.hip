@@ -168,7 +168,10 @@ __device__ __forceinline__ void put_key(const LogprobArgs& a, uint32_t row, uint
 constexpr uint32_t kMostFound = 1024;
 
 // A workgroup takes one part of one row.
-template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_row(LogprobArgs a)
+//
+// kOnce: logits (and their gradient, in lp_backward) go past the caches.  For tensors of 256 MiB and more, which no cache keeps for whoever reads them
+// next: 4096 x 131072 in 16 bits, both passes, 595 us without and 537 with it.  Smaller ones are left to the caches.
+template <typename T, bool kOnce> __global__ void __launch_bounds__(kLpThreads) lp_row(LogprobArgs a)
 {
     __shared__ Softmax waves[kLpThreads / kWave];
     __shared__ uint64_t best[kLpThreads], rows_best[kLpThreads / 16], list[kMostFound], bound;
@@ -184,7 +187,7 @@ template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_row(Logpr
     float most = -INFINITY;                                  // this thread's maximum, and where it was met first
     uint32_t group = from + t * 8;
     for (uint32_t at = from + t * 8; at < to; at += kLpThreads * 8) {
-        const f32x8 v = load_some(x + at, (int)(to - at), -INFINITY);
+        const f32x8 v = kOnce && to - at >= 8 ? load8_once(x + at) : load_some(x + at, (int)(to - at), -INFINITY);
         const float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
         if (m > most) group = at;
         most = fmaxf(most, m);
@@ -348,7 +351,7 @@ constexpr float kFarLse = 256.f;
 // A workgroup takes a chunk of a row.  Each number is read before the thread that read it writes its gradient, which may go to the same place.
 // An lse beyond 256 (logits around a type's lowest value, say) says too little in 32 bits: the first workgroup of such a row then
 // sums it up again and writes all of it.
-template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_backward(LogprobBackwardArgs a)
+template <typename T, bool kOnce> __global__ void __launch_bounds__(kLpThreads) lp_backward(LogprobBackwardArgs a)
 {
     __shared__ uint32_t words[kLpThreads / kWave];
     __shared__ Softmax waves[kLpThreads / kWave];
@@ -377,7 +380,7 @@ template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_backward(
             const uint32_t at = chunk * kLpChunk + (u * kLpThreads + threadIdx.x) * 8;
             if (at >= a.vocabulary) break;
             const int n = (int)(a.vocabulary - at);
-            const f32x8 v = load_some(x + at, n, -INFINITY);
+            const f32x8 v = kOnce && n >= 8 ? load8_once(x + at) : load_some(x + at, n, -INFINITY);
             f32x8 out;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -388,7 +391,8 @@ template <typename T> __global__ void __launch_bounds__(kLpThreads) lp_backward(
                 if (at + i == (uint32_t)token) r += g;
                 out[i] = nothing ? 0.f : r;
             }
-            store_some(d + at, n, out);
+            if (kOnce && n >= 8) store8_once(d + at, out);
+            else store_some(d + at, n, out);
         }
 }
 
@@ -415,6 +419,8 @@ bool lp_sizes_ok(uint32_t dtype, uint32_t rows, uint32_t vocabulary)
     return dtype <= STALLOC_F16 && rows >= 1 && rows < 0x1000000u && vocabulary >= 1 && vocabulary < 0x40000000u;
 }
 
+bool read_once(uint32_t dtype, uint32_t rows, uint32_t vocabulary) { return (uint64_t)rows * vocabulary * bytes_of(dtype) >= (256u << 20); }
+
 }  // namespace
 
 extern "C" int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vocabulary, const void* logits, uint64_t row_stride,
@@ -436,7 +442,8 @@ extern "C" int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vo
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(lp_row<T>, dim3(rows * shape.parts), dim3(kLpThreads), 0, stream, a);
+        if (read_once(dtype, rows, vocabulary)) hipLaunchKernelGGL((lp_row<T, true>), dim3(rows * shape.parts), dim3(kLpThreads), 0, stream, a);
+        else hipLaunchKernelGGL((lp_row<T, false>), dim3(rows * shape.parts), dim3(kLpThreads), 0, stream, a);
         if (shape.parts > 1) hipLaunchKernelGGL(lp_join<T>, dim3(rows), dim3(kLpThreads), 0, stream, a);
     });
     return launched();
@@ -454,6 +461,10 @@ extern "C" int stalloc_token_logprobs_backward(uint32_t dtype, uint32_t rows, ui
     if ((uint64_t)rows * chunks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     const LogprobBackwardArgs a = {rows, vocabulary, chunks, logits, row_stride, tokens, lse, entropy, d_logprob, d_entropy, d_logits, d_row_stride, device_status};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    with_type(dtype, [&](auto t) { hipLaunchKernelGGL(lp_backward<decltype(t)>, dim3(rows * chunks), dim3(kLpThreads), 0, stream, a); });
+    with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        if (read_once(dtype, rows, vocabulary)) hipLaunchKernelGGL((lp_backward<T, true>), dim3(rows * chunks), dim3(kLpThreads), 0, stream, a);
+        else hipLaunchKernelGGL((lp_backward<T, false>), dim3(rows * chunks), dim3(kLpThreads), 0, stream, a);
+    });
     return launched();
 }

@@ -34,6 +34,13 @@ template <typename T> __device__ __forceinline__ void store8(T* p, f32x8 x)
     const typename Vec<T>::x8 v = __builtin_convertvector(x, typename Vec<T>::x8);
     __builtin_memcpy(p, &v, sizeof(v));
 }
+// The same past the caches: for numbers that nobody reads again before they would be gone from them.
+template <typename T> using Loose = typename Vec<T>::x8 __attribute__((aligned(sizeof(T))));
+template <typename T> __device__ __forceinline__ f32x8 load8_once(const T* p) { return __builtin_convertvector(__builtin_nontemporal_load((const Loose<T>*)p), f32x8); }
+template <typename T> __device__ __forceinline__ void store8_once(T* p, f32x8 x)
+{
+    __builtin_nontemporal_store((Loose<T>)__builtin_convertvector(x, typename Vec<T>::x8), (Loose<T>*)p);
+}
 // The first `n` of eight numbers (n may be 0 or less); `fill` in place of the others.
 template <typename T> __device__ __forceinline__ f32x8 load_some(const T* p, int n, float fill)
 {

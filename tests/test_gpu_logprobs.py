@@ -188,3 +188,24 @@ def test_gradient_against_differences(S):
 
     slope = (loss(x.double() + step * way) - loss(x.double() - step * way)) / (2 * step)
     assert abs(float((b["d_logits"].double().cpu() * way).sum()) - slope) <= 1e-4 * (1.0 + abs(slope))
+
+
+def test_logits_beyond_the_caches(S):
+    """256 MiB and more go past the caches, in rows of an odd number of elements: rows spread over the tensor against the definition, and a
+    gradient in place of the logits."""
+    import torch
+    rows, v = 1400, 100003
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(rows, v, device="cuda", dtype=torch.bfloat16).normal_(0.0, 2.0, generator=gen)
+    tokens = torch.randint(v, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    g = torch.randn(rows, device="cuda", generator=gen)
+    some = torch.tensor([0, 1, 700, 1398, 1399])
+    f = S.stalloc_token_logprobs(x, tokens, top=3)
+    kept = x[some.cuda()].cpu()
+    small = _check(S, kept, tokens.cpu()[some], 3, g.cpu()[some])
+    for name in ("logprob", "entropy", "lse", "top_tokens", "top_logprobs"):
+        a, b = f[name][some.cuda()].double().cpu(), small[name].double().cpu()
+        assert bool(((a - b).abs() <= 2e-6 * (1.0 + b.abs())).all())           # (rows that are few are cut into parts: another order of sums)
+    want = S.stalloc_token_logprobs_backward(x[some.cuda()], tokens[some.cuda()], f["lse"][some.cuda()], f["entropy"][some.cuda()], g[some.cuda()])["d_logits"]
+    back = S.stalloc_token_logprobs_backward(x, tokens, f["lse"], f["entropy"], g, out={"d_logits": x})["d_logits"]
+    assert torch.equal(back[some.cuda()], want)

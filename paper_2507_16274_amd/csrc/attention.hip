@@ -68,7 +68,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
         } else {
             tiles_landed<0>();
         }
-        if (key <= first + 31) {                             // (else none of the wave's rows sees any of these keys)
+        if (key <= first + 31 && first < p.end) {            // (else none of the wave's rows sees any of these keys, or it has no rows)
             f32x16 s[kAttnTiles] = {};
             products<kAttnTiles * kD / 16, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / kAttnTiles, 64 * kD * (i % kAttnTiles)); },
                                                  [&](int i, V8<T> k) { s[i % kAttnTiles] = mma(k, q[i / kAttnTiles], s[i % kAttnTiles]); });

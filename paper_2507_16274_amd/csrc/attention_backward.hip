@@ -98,7 +98,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             }
             const uint32_t along = now * 2 * kTile + places.along, cross = now * 2 * kTile + places.cross;
             const f32x2* stats = ring_stats[now][wave_id()];
-            if (row + kAbStep - 1 >= first) {                // (else none of these rows sees a key of this wave)
+            if (row + kAbStep - 1 >= first && first < p.end) {       // (else none of these rows sees a key of this wave, or it has no keys)
                 f32x16 s = {}, dp = {};
                 products<kD / 8, 3, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                        [&](int i, V8<T> r) {
@@ -193,7 +193,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                 tiles_landed<0>();
             }
             const uint32_t tile = step % kAbStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
-            if (key > first + 31) continue;                  // (none of the wave's rows sees any of these keys)
+            if (key > first + 31 || first >= p.end) continue;        // (none of the wave's rows sees any of these keys, or it has no rows)
             f32x16 s = {}, dp = {};
             products<kD / 8, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                    [&](int i, V8<T> r) {

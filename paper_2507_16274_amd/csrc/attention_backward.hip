@@ -3,8 +3,8 @@
 //     p_ij = exp(scale q_i . k_j - lse_i),  D_i = do_i . o_i,  ds_ij = scale p_ij (do_i . v_j - D_i)
 //     dq_i = sum_j ds_ij k_j,   dk_j = sum_h sum_i ds_ij q_i,   dv_j = sum_h sum_i p_ij do_i
 //
-// Three kernels: D; dk and dv, a workgroup per 128 keys that goes through all rows that see them, of all heads that share them; dq, a workgroup per
-// 128 rows of a head.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave:
+// Two kernels: D and dq, a workgroup per 128 rows of a head; then dk and dv, a workgroup per 128 keys that goes through all rows that see them, of
+// all heads that share them.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave:
 // no atomics, no partial gradients in memory, and the same result every time.
 #include "attention.h"
 
@@ -23,34 +23,8 @@ template <typename T> struct AttentionBackwardArgs {
 
 constexpr int kAbThreads = 256, kAbRows = kPieceRows, kAbStep = 32, kAbStages = 4;
 
-__device__ __forceinline__ float row_sum(float v)
-{
-    v += dpp<kDppRowRor8>(0.f, v);
-    v += dpp<kDppRowRor4>(0.f, v);
-    v += dpp<kDppRowRor2>(0.f, v);
-    v += dpp<kDppRowRor1>(0.f, v);
-    return v;
-}
-
 // lse in units of log 2; a row that saw nothing weighs nothing.
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
-
-// D: 16 lanes take a row of one head.
-template <typename T> __global__ void __launch_bounds__(256) attention_dots(AttentionBackwardArgs<T> a)
-{
-    const uint64_t at = (uint64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    if (at >= (uint64_t)a.tokens * a.heads) return;
-    const uint32_t token = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads), col = (threadIdx.x & 15) * 8;
-    float v = 0.f;
-    if (col < a.head_dim) {
-        const f32x8 x = load8(a.d_o.at(token, head) + col), y = load8(a.o.at(token, head) + col);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v = __builtin_fmaf(x[i], y[i], v);
-    }
-    v = row_sum(v);
-    const uint64_t to = (uint64_t)head * a.tokens + token;
-    if (col == 0) a.stats[to] = f32x2{lse2_of(a.lse[to]), v};
-}
 
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dk_dv(AttentionBackwardArgs<T> a)
 {
@@ -182,7 +156,15 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         V8<T> q[kD / 16], d_o[kD / 16];
         load_row<T, kD, kFull>(q, a.q.at(mine, head), a.head_dim);
         load_row<T, kD, kFull>(d_o, a.d_o.at(mine, head), a.head_dim);
-        const f32x2 stats = a.stats[(uint64_t)head * a.tokens + mine];
+        // D_i of the lane's row, half of the columns each; for the kernel behind this one as well.
+        V8<T> o[kD / 16];
+        load_row<T, kD, kFull>(o, a.o.at(mine, head), a.head_dim);
+        const uint64_t at = (uint64_t)head * a.tokens + mine;
+        f32x2 stats = {lse2_of(a.lse[at]), 0.f};
+#pragma unroll
+        for (int c = 0; c < kD / 16; ++c) stats[1] += dot(__builtin_convertvector(o[c], f32x8), __builtin_convertvector(d_o[c], f32x8));
+        stats[1] += across(stats[1]);
+        if (row < p.end && half == 0) a.stats[at] = stats;
         vector_memory_done();
         for (uint32_t step = 0; step < steps; ++step) {
             const uint32_t key = p.begin + step * kAbStep;
@@ -227,8 +209,8 @@ namespace {
 
 template <typename T, int kD, bool kFull> void launch_backward(const AttentionBackwardArgs<T>& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.keys.pieces * a.keys.heads * a.keys.parts), dim3(kAbThreads), 0, stream, a);
     hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.rows.pieces * a.heads), dim3(kAbThreads), 0, stream, a);
+    hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.keys.pieces * a.keys.heads * a.keys.parts), dim3(kAbThreads), 0, stream, a);
 }
 
 // Parts of the walk over a piece's rows: one, unless the pieces alone do not give every CU two workgroups.  A part leaves 8 bytes for every number of k in
@@ -249,9 +231,9 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
 {
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
     const uint32_t heads = shape->heads, kv = shape->kv_heads, parts = parts_of(shape);
-    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows), rows = ((uint64_t)shape->tokens * heads + 15) / 16;
+    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows);
     const uint64_t joined = 2 * (uint64_t)kv * shape->tokens * shape->head_dim;
-    if (pieces * heads > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || rows > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    if (pieces * heads > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     const bool listed = list_pays(pieces * heads, shape->sequences);
     Carver cv(workspace);
     f32x2* stats = cv.take<f32x2>((size_t)shape->tokens * heads + kAbStep);
@@ -273,7 +255,6 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
             const AttentionBackwardArgs<T> a = {heads_of<T>(d_o), heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), heads_of<T>(dq),
                                                 heads_of<T>(dk), heads_of<T>(dv), lse, stats, device_status, by_rows, by_keys, partial, shape->tokens,
                                                 heads, heads / kv, shape->head_dim, shape->scale};
-            hipLaunchKernelGGL(attention_dots<T>, dim3((uint32_t)rows), dim3(256), 0, stream, a);
             if (shape->head_dim == 128) launch_backward<T, 128, true>(a, stream);
             else if (shape->head_dim > 64) launch_backward<T, 128, false>(a, stream);
             else if (shape->head_dim == 64) launch_backward<T, 64, true>(a, stream);

@@ -103,6 +103,14 @@ __device__ __forceinline__ float wave_max(float v)
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
+__device__ __forceinline__ float dot(f32x8 a, f32x8 b)
+{
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v = __builtin_fmaf(a[i], b[i], v);
+    return v;
+}
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

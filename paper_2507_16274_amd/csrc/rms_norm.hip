@@ -148,14 +148,6 @@ struct NormBackwardArgs {
     float* part;                                             // [teams][width]: sums of d_y * sum * rstd over a team's rows
 };
 
-__device__ __forceinline__ float dot(f32x8 a, f32x8 b)
-{
-    float v = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v = __builtin_fmaf(a[i], b[i], v);
-    return v;
-}
-
 template <typename T> __device__ __forceinline__ void emit_dx(const NormBackwardArgs& a, uint32_t row, uint32_t col, f32x8 g, f32x8 s, f32x8 d_sum, float r, float c)
 {
     store_some((T*)a.dx + (uint64_t)row * a.width + col, (int)(a.width - col), r * (g - s * (r * r * c)) + d_sum);

@@ -62,6 +62,13 @@ template <int kD> struct Places {
     }
 };
 
+// A sum as it is, in a register: merged with the exclusive ors behind it, each of their constants would take a register of its own.
+__device__ __forceinline__ uint32_t kept(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // The A operand of a product over columns 16 c .. + 15 of the rows l % 32 of the tile that lies `tile` bytes behind `ring`.
 template <typename T, int kD> __device__ __forceinline__ V8<T> read_along(const T* ring, uint32_t along_in_tile, int c, uint32_t further = 0)
 {
@@ -167,6 +174,50 @@ template <typename T, int kD, bool kFull> __device__ __forceinline__ void store_
             typedef float f32x4 __attribute__((ext_vector_type(4)));
             const f32x4 v = {x[d][4 * i] * factor, x[d][4 * i + 1] * factor, x[d][4 * i + 2] * factor, x[d][4 * i + 3] * factor};
             if (kFull || col < head_dim) *(V4<T>*)(row + col) = __builtin_convertvector(v, V4<T>);
+        }
+}
+
+// Where a row does not see a key its weight is 0, but 0 times an infinity or a NaN in what the key stands for is none: in the tiles on a piece's diagonal these
+// would reach rows that do not see them.  So a wave whose results are not all finite makes them once more, pair by pair in 32 bits, without the
+// pairs that are masked (rows_again, keys_again).  The check is 64 instructions a wave, less than 1 % of one sequence of 8192.
+template <int kN> __device__ __forceinline__ bool not_finite(const f32x16 (&x)[kN])
+{
+    float t[4] = {};
+#pragma unroll
+    for (int d = 0; d < kN; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i % 4] = __builtin_fmaf(x[d][i], 0.f, t[i % 4]);
+    return (t[0] + t[1]) + (t[2] + t[3]) != 0.f;
+}
+
+// Scalar product of the lane's row (as load_row gives it, half of its columns; the other half is across) and a row in memory.
+template <typename T, int kD, bool kFull> __device__ __forceinline__ float dot_row(const V8<T> (&v)[kD / 16], const T* row, uint32_t head_dim)
+{
+    float sum = 0.f;
+    const uint32_t half = kept(lane_id() >> 5);
+#pragma unroll
+    for (int c = 0; c < kD / 16; ++c) {
+        const uint32_t col = 16 * c + 8 * half;
+        if (kFull || col < head_dim) sum += dot(__builtin_convertvector(v[c], f32x8), load8(row + col));
+        __builtin_amdgcn_sched_barrier(0);                   // (one piece of the row in registers at a time: the walks above have none to spare)
+    }
+    return sum + across(sum);
+}
+
+// x += w * (a row in memory), columns as store_row has them.
+template <typename T, int kD, bool kFull> __device__ __forceinline__ void add_row(f32x16 (&x)[kD / 32], float w, const T* row, uint32_t head_dim)
+{
+    const uint32_t half = kept(lane_id() >> 5);
+#pragma unroll
+    for (int d = 0; d < kD / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t col = 32 * d + 8 * i + 4 * half;
+            if (!kFull && col >= head_dim) continue;
+            const V4<T> v = *(const V4<T>*)(row + col);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[d][4 * i + j] = __builtin_fmaf(w, (float)v[j], x[d][4 * i + j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
 }
 

@@ -20,7 +20,23 @@ template <typename T> struct AttentionArgs {
 
 constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2, kAttnTiles = kAttnKeys / 32;
 
-template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, 2) attention_rows(AttentionArgs<T> a)
+// o of a wave's rows pair by pair (attention.h).  m: their largest scores (scores do not depend on what other keys stand for).
+template <typename T, int kD, bool kFull> __device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piece& p, uint32_t head, float m, f32x16 (&o)[kD / 32])
+{
+    const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
+    const float scale = a.scale * kLog2e;
+    V8<T> q[kD / 16];
+    load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
+#pragma unroll
+    for (int d = 0; d < kD / 32; ++d) o[d] = f32x16{};
+#pragma unroll 1
+    for (uint32_t key = p.begin; key <= umin(first + 31, last); ++key) {
+        const float s = dot_row<T, kD, kFull>(q, a.k.at(key, kv), a.head_dim);
+        if (key <= row) add_row<T, kD, kFull>(o, exp2_fast(__builtin_fmaf(s, scale, -m * scale)), a.v.at(key, kv), a.head_dim);
+    }
+}
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAttnThreads, kD == 64 ? 4 : 2) attention_rows(AttentionArgs<T> a)
 {
     __shared__ __attribute__((aligned(256))) T ring[kAttnStages][2][kAttnKeys * kD];       // keys, values
     if (blockIdx.x == 0 && !a.work.list) check_bounds(a.work.bounds, a.work.sequences, a.work.tokens, a.status);
@@ -61,7 +77,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t key = p.begin + step * kAttnKeys;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
-        const uint32_t tile = step % kAttnStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
+        const uint32_t tile = step % kAttnStages * 2 * kTile, along = kept(tile + places.along), cross = kept(tile + places.cross);
         if (step + kAttnStages - 1 < steps) {
             tiles_landed<2 * Tile::kLoads * (kAttnStages - 2)>();
             fetch(step + kAttnStages - 1);
@@ -118,6 +134,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                                                  [&](int i, V8<T> v) { o[i % kDs] = mma(v, w[i / kDs], o[i % kDs]); });
         }
     }
+    if (__any(not_finite(o))) rows_again<T, kD, kFull>(a, p, head, m, o);
     total += across(total);
     if (row >= p.end) return;
     store_row<T, kD, kFull>(a.o.at(row, head), o, total == 0.f ? 0.f : 1.f / total, a.head_dim);

@@ -26,7 +26,34 @@ constexpr int kAbThreads = 256, kAbRows = kPieceRows, kAbStep = 32, kAbStages = 
 // lse in units of log 2; a row that saw nothing weighs nothing.
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
-template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dk_dv(AttentionBackwardArgs<T> a)
+// dk and dv of a wave's keys pair by pair (attention.h): `steps` steps of the walk from `from_step` on.
+template <typename T, int kD, bool kFull>
+__device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t kv, uint32_t from_step, uint32_t steps, f32x16 (&dk)[kD / 32],
+                                           f32x16 (&dv)[kD / 32])
+{
+    const uint32_t first = p.first + 32 * wave_id(), key = first + (lane_id() & 31), last = p.end - 1, per_head = (p.end - p.first + kAbStep - 1) / kAbStep;
+    V8<T> k[kD / 16], v[kD / 16];
+    load_row<T, kD, kFull>(k, a.k.at(umin(key, last), kv), a.head_dim);
+    load_row<T, kD, kFull>(v, a.v.at(umin(key, last), kv), a.head_dim);
+#pragma unroll
+    for (int d = 0; d < kD / 32; ++d) dk[d] = dv[d] = f32x16{};
+    for (uint32_t step = from_step; step < from_step + steps; ++step) {
+        const uint32_t head = kv * a.group + step / per_head, begin = p.first + step % per_head * kAbStep;
+#pragma unroll 1
+        for (uint32_t row = umax(begin, first); row < umin(begin + kAbStep, p.end); ++row) {
+            const T* q = a.q.at(row, head);
+            const T* d_o = a.d_o.at(row, head);
+            const float s = dot_row<T, kD, kFull>(k, q, a.head_dim), dp = dot_row<T, kD, kFull>(v, d_o, a.head_dim);
+            const f32x2 stats = a.stats[(uint64_t)head * a.tokens + row];
+            const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
+            if (row < key) continue;
+            add_row<T, kD, kFull>(dv, w, d_o, a.head_dim);
+            add_row<T, kD, kFull>(dk, w * (dp - stats[1]) * a.scale, q, a.head_dim);
+        }
+    }
+}
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, kD == 64 ? 3 : 2) attention_dk_dv(AttentionBackwardArgs<T> a)
 {
     __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
     __shared__ f32x2 ring_stats[kAbStages][kAbThreads / kWave][kAbStep];     // (a copy per wave)
@@ -70,7 +97,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             } else {
                 tiles_landed<0>();
             }
-            const uint32_t along = now * 2 * kTile + places.along, cross = now * 2 * kTile + places.cross;
+            const uint32_t along = kept(now * 2 * kTile + places.along), cross = kept(now * 2 * kTile + places.cross);
             const f32x2* stats = ring_stats[now][wave_id()];
             if (row + kAbStep - 1 >= first && first < p.end) {       // (else none of these rows sees a key of this wave, or it has no keys)
                 f32x16 s = {}, dp = {};
@@ -104,6 +131,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             if (row >= p.end) row = p.first;
             now = (now + 1) % kAbStages;
         }
+        if (__any(not_finite(dk) || not_finite(dv))) keys_again<T, kD, kFull>(a, p, kv, from_step, steps, dk, dv);
     }
     if (key >= p.end) return;
     if (parts > 1) {
@@ -128,7 +156,26 @@ template <typename T> __global__ void __launch_bounds__(256) attention_join(Atte
     store8(to.at(row % a.tokens, (uint32_t)(row / a.tokens)) + in % a.head_dim, sum);
 }
 
-template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, 2) attention_dq(AttentionBackwardArgs<T> a)
+// dq of a wave's rows pair by pair (attention.h).
+template <typename T, int kD, bool kFull>
+__device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t head, f32x2 stats, f32x16 (&dq)[kD / 32])
+{
+    const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
+    V8<T> q[kD / 16], d_o[kD / 16];
+    load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
+    load_row<T, kD, kFull>(d_o, a.d_o.at(umin(row, last), head), a.head_dim);
+#pragma unroll
+    for (int d = 0; d < kD / 32; ++d) dq[d] = f32x16{};
+#pragma unroll 1
+    for (uint32_t key = p.begin; key <= umin(first + 31, last); ++key) {
+        const T* k = a.k.at(key, kv);
+        const float s = dot_row<T, kD, kFull>(q, k, a.head_dim), dp = dot_row<T, kD, kFull>(d_o, a.v.at(key, kv), a.head_dim);
+        const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
+        if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - stats[1]) * a.scale, k, a.head_dim);
+    }
+}
+
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, kD == 64 ? 4 : 2) attention_dq(AttentionBackwardArgs<T> a)
 {
     __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // keys, values
     const Task task = take_task<kAbRows, true>(a.rows);
@@ -174,7 +221,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             } else {
                 tiles_landed<0>();
             }
-            const uint32_t tile = step % kAbStages * 2 * kTile, along = tile + places.along, cross = tile + places.cross;
+            const uint32_t tile = step % kAbStages * 2 * kTile, along = kept(tile + places.along), cross = kept(tile + places.cross);
             if (key > first + 31 || first >= p.end) continue;        // (none of the wave's rows sees any of these keys, or it has no rows)
             f32x16 s = {}, dp = {};
             products<kD / 8, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
@@ -197,6 +244,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             products<2 * kDs, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                     [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
+        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, stats, dq);
     }
     if (row < p.end) store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
 }

@@ -33,6 +33,8 @@ def _bounds(lengths):
 def _close(got, want, slack, what):
     import torch
     got = got.double().cpu()
+    if not got.numel():
+        return
     assert torch.equal(torch.isfinite(got), torch.isfinite(want)), what
     fine = torch.isfinite(want)
     assert torch.equal(got[~fine], want[~fine]), what
@@ -263,3 +265,40 @@ def test_batches_whose_pieces_are_listed(S, seed, count, most, pad):
     cuts[2] = n + 5
     bad = torch.tensor(cuts, dtype=torch.int32).cuda()
     assert int(S.stalloc_attention(q, k, v, bad)["status"].item()) == 10
+
+
+@pytest.mark.parametrize("d", [64, 128, 80])
+@pytest.mark.parametrize("at", [0, 1, 31, 32, 70, 127, 128, 199])
+def test_later_tokens_do_not_matter(S, d, at):
+    """NaN and infinities in what a later token stands for reach neither the output nor the gradients of earlier ones: rows that do not see
+    the token at `at`, and keys that it does not see, are what they are without it."""
+    import torch
+    n, h, g = 200, 4, 2
+    t = torch.float16 if at % 2 else torch.bfloat16
+    q, k, v, d_o = _inputs(at + d, n, h, g, d, t)
+    bounds = _bounds([n])
+    _, clean = _check(S, q, k, v, d_o, bounds)
+    want, slack = plain.attention(q, k, v, [0, n], d ** -0.5, d_o)
+    for which, bad in ((1, float("nan")), (2, float("inf")), (2, float("-inf")), (2, float("nan")), (3, float("nan")), (3, float("inf")), (0, float("nan"))):
+        x = [y.clone() for y in (q, k, v, d_o)]
+        x[which][at, 0, 3] = bad
+        f = S.stalloc_attention(*x[:3], bounds)
+        b = S.stalloc_attention_backward(x[3], *x[:3], f["o"], f["lse"], bounds)
+        torch.cuda.synchronize()
+        if which in (1, 2):                                    # k or v of token `at`: rows before it do not see it
+            _close(f["o"][:at], want["o"][:at], slack["o"][:at], "o")
+            _close(b["dq"][:at], want["dq"][:at], slack["dq"][:at], "dq")
+            if which == 2:                                     # v: rows that see it have it where it is, as it is
+                seen = f["o"][at:, :h // g].float().cpu()      # (the heads that read key head 0)
+                assert bool((torch.isnan(seen[:, :, 3]) if bad != bad else seen[:, :, 3] == bad).all())
+                assert bool(torch.isfinite(seen[:, :, [0, 1, 2, 4, 5]]).all()) and bool(torch.isfinite(f["o"][:, h // g:]).all())
+            else:
+                assert bool(torch.isnan(f["o"][at:, :h // g]).all())
+        else:                                                  # q or d_o of row `at`: keys behind it are not seen by it
+            for name in ("dk", "dv"):
+                _close(b[name][at + 1:], want[name][at + 1:], slack[name][at + 1:], name)
+            _close(b["dq"][:at], want["dq"][:at], slack["dq"][:at], "dq")
+            if which == 3:                                     # d_o: keys that the row sees have it in dv
+                got = b["dv"][:at + 1, 0, 3].float().cpu()
+                assert bool((torch.isnan(got) if bad != bad else got == bad).all())
+        assert bool(torch.isfinite(b["dk"][:, 1:]).all()) and bool(torch.isfinite(b["dq"][:, h // g:]).all())      # the other key head

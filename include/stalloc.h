@@ -435,6 +435,9 @@ typedef struct stalloc_attention_shape {
  *                 STALLOC_ERR_BAD_BOUNDS (outputs unspecified, memory-safe).
  *   lse           device [heads][tokens]
  *   device_status device [1], written
+ *   workspace     depends on the whole shape: query it for the shape of the call.  (16 bytes a piece of 128 rows where a batch of several
+ *                 sequences has many; where pieces and heads are few, walks over keys are cut into parts whose sums are kept, up to
+ *                 4 * head_dim + 8 bytes for each of 131072 rows of a head.)
  */
 int stalloc_attention(const stalloc_attention_shape *shape, const stalloc_heads *q, const stalloc_heads *k,
                       const stalloc_heads *v, const uint32_t *bounds, const stalloc_heads *o, float *lse,
@@ -443,7 +446,8 @@ int stalloc_attention(const stalloc_attention_shape *shape, const stalloc_heads 
 /*
  * Gradients of the above for a gradient d_o of its output: dq, dk, dv (those of key heads summed over the
  * heads that read them).  o and lse as written by the forward call.  Weights are computed again from q, k
- * and lse; gradients of padding are 0.
+ * and lse; gradients of padding are 0.  The workspace depends on the whole shape, as above (and 8 bytes for every
+ * row of a head).
  */
 int stalloc_attention_backward(const stalloc_attention_shape *shape, const stalloc_heads *d_o, const stalloc_heads *q,
                                const stalloc_heads *k, const stalloc_heads *v, const stalloc_heads *o, const float *lse,

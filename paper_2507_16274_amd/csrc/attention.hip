@@ -14,14 +14,19 @@ template <typename T> struct AttentionArgs {
     float* lse;
     uint32_t* status;
     Work work;
+    float* partial;                                          // [parts][heads][tokens][head_dim]: sums of a part, if there are several
+    f32x2* part_stats;                                       // [parts][heads][tokens]: largest score and sum of weights of a part
     uint32_t group, head_dim;
     float scale;
 };
 
+// Tiles of a part at least: two more kernels' beginnings and ends are about as long as a few tiles.  One sequence of 4096, 4 heads of 128: 72 us in one part, 39 in four.
+constexpr uint32_t kLeastSteps = 4;
 constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2, kAttnTiles = kAttnKeys / 32;
 
-// o of a wave's rows pair by pair (attention.h).  m: their largest scores (scores do not depend on what other keys stand for).
-template <typename T, int kD, bool kFull> __device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piece& p, uint32_t head, float m, f32x16 (&o)[kD / 32])
+// o of a wave's rows over keys from .. to - 1, pair by pair (attention.h).  m: their largest scores (scores do not depend on what other keys stand for).
+template <typename T, int kD, bool kFull>
+__device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, float m, f32x16 (&o)[kD / 32])
 {
     const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
     const float scale = a.scale * kLog2e;
@@ -30,7 +35,7 @@ template <typename T, int kD, bool kFull> __device__ __forceinline__ void rows_a
 #pragma unroll
     for (int d = 0; d < kD / 32; ++d) o[d] = f32x16{};
 #pragma unroll 1
-    for (uint32_t key = p.begin; key <= umin(first + 31, last); ++key) {
+    for (uint32_t key = from; key < umin(to, umin(first + 31, last) + 1); ++key) {
         const float s = dot_row<T, kD, kFull>(q, a.k.at(key, kv), a.head_dim);
         if (key <= row) add_row<T, kD, kFull>(o, exp2_fast(__builtin_fmaf(s, scale, -m * scale)), a.v.at(key, kv), a.head_dim);
     }
@@ -45,8 +50,12 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     const uint32_t head = task.head;
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
+    const uint32_t parts = a.work.parts, part = task.part;
+    const uint64_t part_row = ((uint64_t)part * a.work.heads + head) * a.work.tokens + row;
     if (p.no_keys) {
-        if (row < p.end) {
+        if (row < p.end && parts > 1) {
+            if (half == 0) a.part_stats[part_row] = f32x2{-1e30f, 0.f};
+        } else if (row < p.end) {
             const f32x16 zero[kD / 32] = {};
             store_row<T, kD, kFull>(a.o.at(row, head), zero, 0.f, a.head_dim);
             if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = -INFINITY;
@@ -60,12 +69,15 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     const Places<kD> places;
     float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
     f32x16 o[kD / 32] = {};
-    const uint32_t steps = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
+    // The walk: tiles of keys up to the last row's; this part's share of them.
+    const uint32_t all = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
+    const uint32_t from = p.begin + (uint32_t)((uint64_t)all * part / parts) * kAttnKeys;
+    const uint32_t steps = (uint32_t)((uint64_t)all * (part + 1) / parts) - (from - p.begin) / kAttnKeys;
     using Tile = Rows<T, kD, kAttnKeys, kAttnThreads, kFull>;
     const auto fetch = [&](uint32_t step) {
         T (&stage)[2][kAttnKeys * kD] = ring[step % kAttnStages];
-        Tile::fetch(stage[0], k, a.k.token, p.begin + step * kAttnKeys, last, a.head_dim);
-        Tile::fetch(stage[1], v, a.v.token, p.begin + step * kAttnKeys, last, a.head_dim);
+        Tile::fetch(stage[0], k, a.k.token, from + step * kAttnKeys, last, a.head_dim);
+        Tile::fetch(stage[1], v, a.v.token, from + step * kAttnKeys, last, a.head_dim);
     };
     if (!kFull) clear_lds<sizeof(ring) / 4, kAttnThreads>(ring);
 #pragma unroll
@@ -75,7 +87,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
     vector_memory_done();                                    // (q is here before the loop: its loads are not waited for among the tiles')
     for (uint32_t step = 0; step < steps; ++step) {
-        const uint32_t key = p.begin + step * kAttnKeys;
+        const uint32_t key = from + step * kAttnKeys;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
         const uint32_t tile = step % kAttnStages * 2 * kTile, along = kept(tile + places.along), cross = kept(tile + places.cross);
         if (step + kAttnStages - 1 < steps) {
@@ -134,11 +146,39 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                                                  [&](int i, V8<T> v) { o[i % kDs] = mma(v, w[i / kDs], o[i % kDs]); });
         }
     }
-    if (__any(not_finite(o))) rows_again<T, kD, kFull>(a, p, head, m, o);
+    if (__any(not_finite(o))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAttnKeys, m, o);
     total += across(total);
     if (row >= p.end) return;
+    if (parts > 1) {
+        if (half == 0) a.part_stats[part_row] = f32x2{m, total};
+        if (steps) store_row<float, kD, kFull>(a.partial + part_row * a.head_dim, o, 1.f, a.head_dim);
+        return;
+    }
     store_row<T, kD, kFull>(a.o.at(row, head), o, total == 0.f ? 0.f : 1.f / total, a.head_dim);
     if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = (m * scale + log2f(total)) * kLn2;
+}
+
+// o and lse from the parts': eight columns of a row a thread.
+template <typename T> __global__ void __launch_bounds__(256) attention_join(AttentionArgs<T> a)
+{
+    const uint32_t pieces = a.head_dim / 8;
+    const uint64_t rows = (uint64_t)a.work.heads * a.work.tokens, at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / pieces;
+    const uint32_t col = (uint32_t)(at % pieces) * 8;
+    if (row >= rows) return;
+    const float scale = a.scale * kLog2e;
+    float m = -1e30f, total = 0.f;
+    for (uint32_t part = 0; part < a.work.parts; ++part) m = fmaxf(m, a.part_stats[part * rows + row][0]);
+    f32x8 o = {};
+    for (uint32_t part = 0; part < a.work.parts; ++part) {
+        const f32x2 stats = a.part_stats[part * rows + row];
+        if (stats[1] == 0.f) continue;                       // (saw nothing: its sums may not be there)
+        const float f = exp2_fast((stats[0] - m) * scale);
+        total += stats[1] * f;
+        o += load8(a.partial + (part * rows + row) * a.head_dim + col) * f;
+    }
+    const uint32_t head = (uint32_t)(row / a.work.tokens), token = (uint32_t)(row % a.work.tokens);
+    store8(a.o.at(token, head) + col, o * (total == 0.f ? 0.f : 1.f / total));
+    if (col == 0) a.lse[row] = total == 0.f ? -INFINITY : (m * scale + log2f(total)) * kLn2;
 }
 
 // All pieces of the batch, those with the longest walks first: counted by length (of their walk, in pieces), placed by count.  One workgroup; a wave takes a
@@ -225,9 +265,13 @@ extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const sta
                                  uint32_t* device_status, void* workspace, size_t* workspace_bytes, void* hip_stream)
 {
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
-    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAttnRows), blocks = pieces * shape->heads;
+    const uint32_t parts = parts_of(row_pieces(shape) * shape->heads, average_rows(shape) / kAttnKeys, kLeastSteps, 8);
+    const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAttnRows), blocks = pieces * shape->heads * parts;
+    const uint64_t rows = (uint64_t)shape->tokens * shape->heads;
     if (blocks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     Carver cv(workspace);
+    float* partial = cv.take<float>(parts > 1 ? parts * rows * shape->head_dim : 0);
+    f32x2* part_stats = cv.take<f32x2>(parts > 1 ? parts * rows : 0);
     uint4* list = cv.take<uint4>(list_pays(blocks, shape->sequences) ? pieces : 1);
     if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
     if (!heads_ok(q, shape, shape->heads, false) || !heads_ok(k, shape, shape->kv_heads, false) || !heads_ok(v, shape, shape->kv_heads, false) ||
@@ -240,9 +284,10 @@ extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const sta
         using T = decltype(t);
         if constexpr (sizeof(T) == 2) {
             const AttentionArgs<T> a = {heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), lse, device_status,
-                                        {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, shape->heads, 1},
-                                        shape->heads / shape->kv_heads, shape->head_dim, shape->scale};
+                                        {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, shape->heads, parts},
+                                        partial, part_stats, shape->heads / shape->kv_heads, shape->head_dim, shape->scale};
             launch_attention<T>(shape, a, (uint32_t)blocks, stream);
+            if (parts > 1) hipLaunchKernelGGL(attention_join<T>, dim3((uint32_t)((rows * (shape->head_dim / 8) + 255) / 256)), dim3(256), 0, stream, a);
         }
     });
     return launched();

@@ -17,10 +17,13 @@ template <typename T> struct AttentionBackwardArgs {
     uint32_t* status;
     Work rows, keys;                                         // shared out for dq; for dk and dv
     float* partial;                                          // [parts][2][kv_heads][tokens][head_dim]: dk, dv of a part, if there are several
+    float* partial_dq;                                       // [parts][heads][tokens][head_dim]
     uint32_t tokens, heads, group, head_dim;
     float scale;
 };
 
+// Tiles of a part at least: of the walk over rows (which goes through several heads, so its parts are few tiles of each), of the walk over keys.
+constexpr uint32_t kLeastRowSteps = 2, kLeastKeySteps = 4;
 constexpr int kAbThreads = 256, kAbRows = kPieceRows, kAbStep = 32, kAbStages = 4;
 
 // lse in units of log 2; a row that saw nothing weighs nothing.
@@ -144,21 +147,22 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     store_row<T, kD, kFull>(a.dv.at(key, kv), dv, 1.f, a.head_dim);
 }
 
-// dk and dv from those of the parts, added up in their order: eight numbers a thread.
-template <typename T> __global__ void __launch_bounds__(256) attention_join(AttentionBackwardArgs<T> a)
+// Tensors of `heads` heads from those of the parts, added up in their order: eight numbers a thread.  kTwo: two tensors, one behind the other in
+// every part (dk, dv).
+template <typename T, bool kTwo> __global__ void __launch_bounds__(256) gradient_join(const float* partial, uint32_t parts, uint32_t heads, uint32_t tokens, uint32_t head_dim, Heads<T> x, Heads<T> y)
 {
-    const uint64_t each = (uint64_t)a.keys.heads * a.tokens * a.head_dim, at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (at >= 2 * each) return;
-    f32x8 sum = load8(a.partial + at);
-    for (uint32_t part = 1; part < a.keys.parts; ++part) sum += load8(a.partial + 2 * part * each + at);
-    const uint64_t in = at < each ? at : at - each, row = in / a.head_dim;
-    const Heads<T>& to = at < each ? a.dk : a.dv;
-    store8(to.at(row % a.tokens, (uint32_t)(row / a.tokens)) + in % a.head_dim, sum);
+    const uint64_t each = (uint64_t)heads * tokens * head_dim, all = kTwo ? 2 * each : each, at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= all) return;
+    f32x8 sum = load8(partial + at);
+    for (uint32_t part = 1; part < parts; ++part) sum += load8(partial + part * all + at);
+    const uint64_t in = at < each ? at : at - each, row = in / head_dim;
+    const Heads<T>& to = at < each ? x : y;
+    store8(to.at(row % tokens, (uint32_t)(row / tokens)) + in % head_dim, sum);
 }
 
-// dq of a wave's rows pair by pair (attention.h).
+// dq of a wave's rows over keys from .. to - 1, pair by pair (attention.h).
 template <typename T, int kD, bool kFull>
-__device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t head, f32x2 stats, f32x16 (&dq)[kD / 32])
+__device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, f32x2 stats, f32x16 (&dq)[kD / 32])
 {
     const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
     V8<T> q[kD / 16], d_o[kD / 16];
@@ -167,7 +171,7 @@ __device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, co
 #pragma unroll
     for (int d = 0; d < kD / 32; ++d) dq[d] = f32x16{};
 #pragma unroll 1
-    for (uint32_t key = p.begin; key <= umin(first + 31, last); ++key) {
+    for (uint32_t key = from; key < umin(to, umin(first + 31, last) + 1); ++key) {
         const T* k = a.k.at(key, kv);
         const float s = dot_row<T, kD, kFull>(q, k, a.head_dim), dp = dot_row<T, kD, kFull>(d_o, a.v.at(key, kv), a.head_dim);
         const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
@@ -175,7 +179,7 @@ __device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, co
     }
 }
 
-template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, kD == 64 ? 4 : 2) attention_dq(AttentionBackwardArgs<T> a)
+template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, kD == 64 ? 3 : 2) attention_dq(AttentionBackwardArgs<T> a)
 {
     __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // keys, values
     const Task task = take_task<kAbRows, true>(a.rows);
@@ -192,11 +196,14 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
         const Places<kD> places;
-        const uint32_t steps = (umin(p.first + kAbRows, p.end) - p.begin + kAbStep - 1) / kAbStep;
+        // The walk: tiles of keys up to the last row's; this part's share of them.
+        const uint32_t all = (umin(p.first + kAbRows, p.end) - p.begin + kAbStep - 1) / kAbStep;
+        const uint32_t from = p.begin + (uint32_t)((uint64_t)all * task.part / a.rows.parts) * kAbStep;
+        const uint32_t steps = (uint32_t)((uint64_t)all * (task.part + 1) / a.rows.parts) - (from - p.begin) / kAbStep;
         const auto fetch = [&](uint32_t step) {
             T (&stage)[2][kAbStep * kD] = ring[step % kAbStages];
-            Tile::fetch(stage[0], k, a.k.token, p.begin + step * kAbStep, last, a.head_dim);
-            Tile::fetch(stage[1], v, a.v.token, p.begin + step * kAbStep, last, a.head_dim);
+            Tile::fetch(stage[0], k, a.k.token, from + step * kAbStep, last, a.head_dim);
+            Tile::fetch(stage[1], v, a.v.token, from + step * kAbStep, last, a.head_dim);
         };
         if (!kFull) clear_lds<sizeof(ring) / 4, kAbThreads>(ring);
         for (uint32_t step = 0; step < kAbStages - 1 && step < steps; ++step) fetch(step);
@@ -211,10 +218,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
 #pragma unroll
         for (int c = 0; c < kD / 16; ++c) stats[1] += dot(__builtin_convertvector(o[c], f32x8), __builtin_convertvector(d_o[c], f32x8));
         stats[1] += across(stats[1]);
-        if (row < p.end && half == 0) a.stats[at] = stats;
+        if (row < p.end && half == 0 && task.part == 0) a.stats[at] = stats;
         vector_memory_done();
         for (uint32_t step = 0; step < steps; ++step) {
-            const uint32_t key = p.begin + step * kAbStep;
+            const uint32_t key = from + step * kAbStep;
             if (step + kAbStages - 1 < steps) {
                 tiles_landed<2 * Tile::kLoads * (kAbStages - 2)>();
                 fetch(step + kAbStages - 1);
@@ -244,9 +251,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             products<2 * kDs, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                     [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
-        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, stats, dq);
+        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, stats, dq);
     }
-    if (row < p.end) store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
+    if (row >= p.end) return;
+    if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, 1.f, a.head_dim);
+    else store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
 }
 
 }  // namespace stalloc
@@ -257,16 +266,17 @@ namespace {
 
 template <typename T, int kD, bool kFull> void launch_backward(const AttentionBackwardArgs<T>& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.rows.pieces * a.heads), dim3(kAbThreads), 0, stream, a);
+    hipLaunchKernelGGL((attention_dq<T, kD, kFull>), dim3(a.rows.pieces * a.heads * a.rows.parts), dim3(kAbThreads), 0, stream, a);
     hipLaunchKernelGGL((attention_dk_dv<T, kD, kFull>), dim3(a.keys.pieces * a.keys.heads * a.keys.parts), dim3(kAbThreads), 0, stream, a);
 }
 
-// Parts of the walk over a piece's rows: one, unless the pieces alone do not give every CU two workgroups.  A part leaves 8 bytes for every number of k in
-// the workspace, which are written and read once.
-uint32_t parts_of(const stalloc_attention_shape* s)
+template <typename T> void launch_joins(const AttentionBackwardArgs<T>& a, hipStream_t stream)
 {
-    const uint64_t pieces = ((uint64_t)s->tokens + kAbRows - 1) / kAbRows * s->kv_heads;
-    return pieces >= 512 ? 1 : umin_host(8, (uint32_t)((512 + pieces - 1) / pieces));
+    const auto blocks = [&](uint32_t heads) { return dim3((uint32_t)(((uint64_t)heads * a.tokens * a.head_dim / 8 + 255) / 256)); };
+    if (a.rows.parts > 1)
+        hipLaunchKernelGGL((gradient_join<T, false>), blocks(a.heads), dim3(256), 0, stream, a.partial_dq, a.rows.parts, a.heads, a.tokens, a.head_dim, a.dq, a.dq);
+    if (a.keys.parts > 1)
+        hipLaunchKernelGGL((gradient_join<T, true>), blocks(2 * a.keys.heads), dim3(256), 0, stream, a.partial, a.keys.parts, a.keys.heads, a.tokens, a.head_dim, a.dk, a.dv);
 }
 
 }  // namespace
@@ -278,15 +288,18 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
                                           size_t* workspace_bytes, void* hip_stream)
 {
     if (!shape_ok(shape) || !workspace_bytes) return STALLOC_ERR_INVALID_ARG;
-    const uint32_t heads = shape->heads, kv = shape->kv_heads, parts = parts_of(shape);
+    const uint32_t heads = shape->heads, kv = shape->kv_heads;
+    const uint32_t parts = parts_of(row_pieces(shape) * kv, average_rows(shape) / kAbStep * (heads / kv), kLeastRowSteps, 16);
+    const uint32_t row_parts = parts_of(row_pieces(shape) * heads, average_rows(shape) / kAbStep, kLeastKeySteps, 8);
     const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows);
     const uint64_t joined = 2 * (uint64_t)kv * shape->tokens * shape->head_dim;
-    if (pieces * heads > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    if (pieces * heads * row_parts > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     const bool listed = list_pays(pieces * heads, shape->sequences);
     Carver cv(workspace);
     f32x2* stats = cv.take<f32x2>((size_t)shape->tokens * heads + kAbStep);
     uint4* list = cv.take<uint4>(listed ? pieces : 0);
     float* partial = cv.take<float>(parts > 1 ? parts * joined : 0);
+    float* partial_dq = cv.take<float>(row_parts > 1 ? (uint64_t)row_parts * heads * shape->tokens * shape->head_dim : 0);
     if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
     if (!heads_ok(d_o, shape, heads, false) || !heads_ok(q, shape, heads, false) || !heads_ok(k, shape, kv, false) || !heads_ok(v, shape, kv, false) ||
         !heads_ok(o, shape, heads, false) || !heads_ok(dq, shape, heads, true) || !heads_ok(dk, shape, kv, true) || !heads_ok(dv, shape, kv, true) ||
@@ -295,19 +308,19 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (listed) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);
     else list = nullptr;
-    const Work by_rows = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, heads, 1};
+    const Work by_rows = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, heads, row_parts};
     const Work by_keys = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, kv, parts};
     with_type(shape->dtype, [&](auto t) {
         using T = decltype(t);
         if constexpr (sizeof(T) == 2) {
             const AttentionBackwardArgs<T> a = {heads_of<T>(d_o), heads_of<T>(q), heads_of<T>(k), heads_of<T>(v), heads_of<T>(o), heads_of<T>(dq),
-                                                heads_of<T>(dk), heads_of<T>(dv), lse, stats, device_status, by_rows, by_keys, partial, shape->tokens,
+                                                heads_of<T>(dk), heads_of<T>(dv), lse, stats, device_status, by_rows, by_keys, partial, partial_dq, shape->tokens,
                                                 heads, heads / kv, shape->head_dim, shape->scale};
             if (shape->head_dim == 128) launch_backward<T, 128, true>(a, stream);
             else if (shape->head_dim > 64) launch_backward<T, 128, false>(a, stream);
             else if (shape->head_dim == 64) launch_backward<T, 64, true>(a, stream);
             else launch_backward<T, 64, false>(a, stream);
-            if (parts > 1) hipLaunchKernelGGL(attention_join<T>, dim3((uint32_t)((joined / 8 + 255) / 256)), dim3(256), 0, stream, a);
+            launch_joins<T>(a, stream);
         }
     });
     return launched();

@@ -61,6 +61,13 @@ template <typename T> __device__ __forceinline__ typename Vec<T>::x8 packed_some
             if (i < n) v[i] = p[i];
     return v;
 }
+// Both for numbers that nobody reads again soon (kOnce: past the caches).
+template <bool kOnce, typename T> __device__ __forceinline__ f32x8 load_some_once(const T* p, int n, float fill) { return kOnce && n >= 8 ? load8_once(p) : load_some(p, n, fill); }
+template <bool kOnce, typename T> __device__ __forceinline__ typename Vec<T>::x8 packed_some_once(const T* p, int n)
+{
+    if (kOnce && n >= 8) return __builtin_nontemporal_load((const Loose<T>*)p);
+    return packed_some(p, n);
+}
 template <typename T> __device__ __forceinline__ void store_some(T* p, int n, f32x8 x)
 {
     if (n >= 8) { store8(p, x); return; }

@@ -88,15 +88,18 @@ template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const 
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// 16 (or 4) bytes per lane from memory to LDS, lane after lane from `lds` on; `base` and `lds` are the same in all lanes.  Written out because
+// 16 bytes per lane from memory to LDS, lane after lane from `lds` on; `base` and `lds` are the same in all lanes.  Written out because
 // the compiler, which cannot know that the tile asked for is not the one read next, would wait for it there and then; what waits
 // for it is tiles_landed.  Nothing is returned in registers.
-template <int kBytes> __device__ __forceinline__ void memory_to_lds(uint32_t lds, const void* base, uint32_t offset)
+__device__ __forceinline__ void memory_to_lds(uint32_t lds, const void* base, uint32_t offset)
 {
-    static_assert(kBytes == 16 || kBytes == 4, "16 or 4 bytes a lane");
     const uint64_t from = uniform((uint64_t)base);
-    if (kBytes == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+// The same, 4 bytes from an address of each lane's own.
+__device__ __forceinline__ void words_to_lds(uint32_t lds, const void* from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return uniform((uint32_t)(size_t)(__attribute__((address_space(3))) const void*)p); }
 
@@ -114,7 +117,7 @@ template <typename T, int kD, int kRows, int kThreads, bool kFull> struct Rows {
 #pragma unroll
         for (int s = 0; s < kLoads; ++s) {
             const uint32_t at = s * kThreads + threadIdx.x, row = at / kPieces, piece = (at % kPieces) ^ turn_of<kD>(row);
-            if (kFull || piece * 8 < head_dim) memory_to_lds<16>(lds + s * kThreads * 16, base, umin(row, most) * bytes + piece * 16);
+            if (kFull || piece * 8 < head_dim) memory_to_lds(lds + s * kThreads * 16, base, umin(row, most) * bytes + piece * 16);
         }
     }
 };

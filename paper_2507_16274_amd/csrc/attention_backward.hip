@@ -15,7 +15,7 @@ namespace stalloc {
 template <typename T> struct AttentionBackwardArgs {
     Heads<T> d_o, q, k, v, o, dq, dk, dv;
     const float* lse;
-    f32x2* stats;                                            // [heads][tokens]: lse in units of log 2, D
+    float* stats;                                            // [heads][2][tokens]: lse in units of log 2, -D
     uint32_t* status;
     Work rows, keys;                                         // shared out for dq; for dk and dv
     float* partial;                                          // [parts][2][kv_heads][tokens][head_dim]: dk, dv of a part, if there are several
@@ -41,6 +41,9 @@ template <typename T, int s> __device__ __forceinline__ V8<T> left_of(const f32x
     return __builtin_convertvector(v - __builtin_convertvector(rounded, f32x8), V8<T>);
 }
 
+// What the loops leave out: dp - D is made by the products, whose sum begins at -D, and scale is multiplied in when results are stored (that and the sums' own beginning are
+// 32 of 160 vector operations a step; one sequence of 4096 with 32 heads of 128: 623 us both passes with them, 603 without).
+
 // lse in units of log 2; a row that saw nothing weighs nothing.
 __device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
@@ -62,11 +65,11 @@ __device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, co
             const T* q = a.q.at(row, head);
             const T* d_o = a.d_o.at(row, head);
             const float s = dot_row<T, kD, kFull>(k, q, a.head_dim), dp = dot_row<T, kD, kFull>(v, d_o, a.head_dim);
-            const f32x2 stats = a.stats[(uint64_t)head * a.tokens + row];
+            const float* stats = a.stats + (uint64_t)head * 2 * a.tokens + row;
             const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
             if (row < key) continue;
             add_row<T, kD, kFull>(dv, w, d_o, a.head_dim);
-            add_row<T, kD, kFull>(dk, w * (dp - stats[1]) * a.scale, q, a.head_dim);
+            add_row<T, kD, kFull>(dk, w * (dp + stats[a.tokens]), q, a.head_dim);
         }
     }
 }
@@ -74,7 +77,7 @@ __device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, co
 template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbThreads, kD == 64 ? 3 : 2) attention_dk_dv(AttentionBackwardArgs<T> a)
 {
     __shared__ __attribute__((aligned(256))) T ring[kAbStages][2][kAbStep * kD];           // rows of q, of d_o
-    __shared__ f32x2 ring_stats[kAbStages][kAbThreads / kWave][kAbStep];     // (a copy per wave)
+    __shared__ __attribute__((aligned(16))) float ring_stats[kAbStages][kAbThreads / kWave][2][kAbStep];     // (a copy per wave)
     if (blockIdx.x == 0 && !a.keys.list) check_bounds(a.keys.bounds, a.keys.sequences, a.tokens, a.status);
     const Task task = take_task<kAbRows, false>(a.keys);
     const Piece p = task.piece;
@@ -92,10 +95,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const uint32_t per_head = (p.end - p.first + kAbStep - 1) / kAbStep, all = per_head * a.group;
         const uint32_t from_step = (uint32_t)((uint64_t)all * task.part / parts), steps = (uint32_t)((uint64_t)all * (task.part + 1) / parts) - from_step;
         uint32_t next_head = kv * a.group + from_step / per_head, next_row = p.first + from_step % per_head * kAbStep, next_slot = 0;
+        const float* lane_stats = a.stats + (uint64_t)half * a.tokens + (lane_id() & 31);
         const auto fetch = [&]() {
             Tile::fetch(ring[next_slot][0], a.q.at(0, next_head), a.q.token, next_row, last, a.head_dim);
             Tile::fetch(ring[next_slot][1], a.d_o.at(0, next_head), a.d_o.token, next_row, last, a.head_dim);
-            memory_to_lds<4>(lds_address(ring_stats[next_slot][wave_id()]), a.stats + (uint64_t)next_head * a.tokens + next_row, lane_id() * 4);
+            words_to_lds(lds_address(ring_stats[next_slot][wave_id()]), lane_stats + (uint64_t)next_head * 2 * a.tokens + next_row);
             next_row += kAbStep;
             if (next_row >= p.end) { next_row = p.first; ++next_head; }
             next_slot = (next_slot + 1) % kAbStages;
@@ -118,9 +122,13 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                     tiles_landed<0>();
                 }
                 const uint32_t along = kept(now * 2 * kTile + places.along), cross = kept(now * 2 * kTile + places.cross);
-                const f32x2* stats = ring_stats[now][wave_id()];
+                const float (*stats)[kAbStep] = ring_stats[now][wave_id()];
                 if (row + kAbStep - 1 >= first && first < p.end) {       // (else none of these rows sees a key of this wave, or it has no keys)
-                    f32x16 s = {}, dp = {};
+                    f32x16 s = {}, dp;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) dp[i + j] = (*(const Vec<float>::x4*)&stats[1][row_of(i, half)])[j];
                     products<kD / 8, 3, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                            [&](int i, V8<T> r) {
                                                if (i % 2 == 0) s = mma(r, k[i / 2], s);
@@ -128,10 +136,13 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                                            });
                     const bool crosses = row < first + 31 || row + kAbStep > p.end;      // some of these rows do not see some of these keys, or are not the sequence's
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const f32x2 st = stats[row_of(i, half)];
-                        s[i] = exp2_fast(__builtin_fmaf(s[i], scale, -st[0]));
-                        dp[i] = s[i] * (dp[i] - st[1]) * a.scale;
+                    for (int i = 0; i < 16; i += 4) {
+                        const Vec<float>::x4 lse2 = *(const Vec<float>::x4*)&stats[0][row_of(i, half)];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            s[i + j] = exp2_fast(__builtin_fmaf(s[i + j], scale, -lse2[j]));
+                            dp[i + j] *= s[i + j];
+                        }
                     }
                     if (crosses)
 #pragma unroll
@@ -164,11 +175,11 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     if (key >= p.end) return;
     if (parts > 1) {
         const uint64_t heads = a.keys.heads, to = ((2 * task.part * heads + kv) * a.tokens + key) * a.head_dim;
-        store_row<float, kD, kFull>(a.partial + to, dk, 1.f, a.head_dim);
+        store_row<float, kD, kFull>(a.partial + to, dk, a.scale, a.head_dim);
         store_row<float, kD, kFull>(a.partial + to + heads * a.tokens * a.head_dim, dv, 1.f, a.head_dim);
         return;
     }
-    store_row<T, kD, kFull>(a.dk.at(key, kv), dk, 1.f, a.head_dim);
+    store_row<T, kD, kFull>(a.dk.at(key, kv), dk, a.scale, a.head_dim);
     store_row<T, kD, kFull>(a.dv.at(key, kv), dv, 1.f, a.head_dim);
 }
 
@@ -200,7 +211,7 @@ __device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, co
         const T* k = a.k.at(key, kv);
         const float s = dot_row<T, kD, kFull>(q, k, a.head_dim), dp = dot_row<T, kD, kFull>(d_o, a.v.at(key, kv), a.head_dim);
         const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
-        if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - stats[1]) * a.scale, k, a.head_dim);
+        if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - stats[1]), k, a.head_dim);
     }
 }
 
@@ -267,14 +278,15 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         // D_i of the lane's row, half of the columns each; for the kernel behind this one as well.
         V8<T> o[kD / 16];
         load_row<T, kD, kFull>(o, a.o.at(mine, head), a.head_dim);
-        const uint64_t at = (uint64_t)head * a.tokens + mine;
-        f32x2 stats = {lse2_of(a.lse[at]), 0.f};
+        f32x2 stats = {lse2_of(a.lse[(uint64_t)head * a.tokens + mine]), 0.f};
 #pragma unroll
         for (int c = 0; c < kD / 16; ++c) stats[1] += dot(__builtin_convertvector(o[c], f32x8), __builtin_convertvector(d_o[c], f32x8));
         stats[1] += across(stats[1]);
         const bool early = p.first == p.begin;
         if (early) stats[1] = early_d<T, kD, kFull>(a, p, kv, q, d_o, stats[0]);
-        if (row < p.end && half == 0 && task.part == 0) a.stats[at] = stats;
+        if (row < p.end && task.part == 0) a.stats[((uint64_t)head * 2 + half) * a.tokens + row] = half == 0 ? stats[0] : -stats[1];
+        f32x16 less_d = f32x16{} - stats[1];
+        asm volatile("" : "+v"(less_d));                     // (in registers, not made anew every step)
         vector_memory_done();
         for (uint32_t step = 0; step < steps; ++step) {
             const uint32_t key = from + step * kAbStep;
@@ -286,7 +298,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             }
             const uint32_t tile = step % kAbStages * 2 * kTile, along = kept(tile + places.along), cross = kept(tile + places.cross);
             if (key > first + 31 || first >= p.end) continue;        // (none of the wave's rows sees any of these keys, or it has no rows)
-            f32x16 s = {}, dp = {};
+            f32x16 s = {}, dp = less_d;
             products<kD / 8, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                    [&](int i, V8<T> r) {
                                        if (i % 2 == 0) s = mma(r, q[i / 2], s);
@@ -295,8 +307,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const bool crosses = key + 31 > first;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float w = exp2_fast(__builtin_fmaf(s[i], scale, -stats[0]));
-                dp[i] = w * (dp[i] - stats[1]) * a.scale;
+                dp[i] *= exp2_fast(__builtin_fmaf(s[i], scale, -stats[0]));
             }
             if (crosses)
 #pragma unroll
@@ -315,8 +326,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, stats, dq);
     }
     if (row >= p.end) return;
-    if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, 1.f, a.head_dim);
-    else store_row<T, kD, kFull>(a.dq.at(row, head), dq, 1.f, a.head_dim);
+    if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, a.scale, a.head_dim);
+    else store_row<T, kD, kFull>(a.dq.at(row, head), dq, a.scale, a.head_dim);
 }
 
 }  // namespace stalloc
@@ -357,7 +368,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
     if (pieces * heads * row_parts > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     const bool listed = list_pays(pieces * heads, shape->sequences);
     Carver cv(workspace);
-    f32x2* stats = cv.take<f32x2>((size_t)shape->tokens * heads + kAbStep);
+    float* stats = cv.take<float>(2 * (size_t)shape->tokens * heads + kAbStep);
     uint4* list = cv.take<uint4>(listed ? pieces : 0);
     float* partial = cv.take<float>(parts > 1 ? parts * joined : 0);
     float* partial_dq = cv.take<float>(row_parts > 1 ? (uint64_t)row_parts * heads * shape->tokens * shape->head_dim : 0);

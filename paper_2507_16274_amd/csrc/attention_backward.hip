@@ -87,7 +87,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     f32x16 dk[kD / 32] = {}, dv[kD / 32] = {};
     if (!p.no_keys) {
         const uint32_t last = p.end - 1;
-        const float scale = a.scale * kLog2e;
+        const float scale = uniform(a.scale * kLog2e);
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
         const Places<kD> places;
@@ -129,7 +129,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                     for (int i = 0; i < 16; i += 4)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) dp[i + j] = (*(const Vec<float>::x4*)&stats[1][row_of(i, half)])[j];
-                    products<kD / 8, 3, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
+                    products<kD / 8, 3, T, 1>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                            [&](int i, V8<T> r) {
                                                if (i % 2 == 0) s = mma(r, k[i / 2], s);
                                                else dp = mma(r, v[i / 2], dp);
@@ -154,10 +154,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                     const V8<T> w[2] = {operand<T, 0>(s), operand<T, 1>(s)}, ds[2] = {operand<T, 0>(dp), operand<T, 1>(dp)};
                     if (early && row < p.begin + kAbRows) {
                         const V8<T> left[2] = {left_of<T, 0>(dp, ds[0]), left_of<T, 1>(dp, ds[1])};
-                        products<kD / 16, 2, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i / 2, i % 2 * 32 * kD); },
+                        products<kD / 16, 2, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i / 2, i % 2 * 32 * kD); },
                                                 [&](int i, V8<T> r) { dk[i / 2] = mma(r, left[i % 2], dk[i / 2]); });
                     }
-                    products<kD / 8, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i / 4, i % 2 * kTile + i / 2 % 2 * 32 * kD); },
+                    products<kD / 8, 4, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i / 4, i % 2 * kTile + i / 2 % 2 * 32 * kD); },
                                            [&](int i, V8<T> r) {
                                                if (i % 2 == 0) dk[i / 4] = mma(r, ds[i / 2 % 2], dk[i / 4]);
                                                else dv[i / 4] = mma(r, w[i / 2 % 2], dv[i / 4]);
@@ -221,7 +221,7 @@ template <typename T, int kD, bool kFull>
 __device__ __forceinline__ float early_d(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t kv, const V8<T> (&q)[kD / 16], const V8<T> (&d_o)[kD / 16], float lse2)
 {
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1;
-    const float scale = a.scale * kLog2e;
+    const float scale = uniform(a.scale * kLog2e);
     float sum = 0.f;
 #pragma unroll 1
     for (uint32_t key = p.begin; key <= umin(first, last); key += 32) {
@@ -257,7 +257,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         const uint32_t last = p.end - 1, kv = head / a.group, mine = umin(row, last);
         const T* k = a.k.at(0, kv);
         const T* v = a.v.at(0, kv);
-        const float scale = a.scale * kLog2e;
+        const float scale = uniform(a.scale * kLog2e);
         using Tile = Rows<T, kD, kAbStep, kAbThreads, kFull>;
         constexpr uint32_t kTile = sizeof(ring[0][0]);
         const Places<kD> places;
@@ -299,7 +299,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const uint32_t tile = step % kAbStages * 2 * kTile, along = kept(tile + places.along), cross = kept(tile + places.cross);
             if (key > first + 31 || first >= p.end) continue;        // (none of the wave's rows sees any of these keys, or it has no rows)
             f32x16 s = {}, dp = less_d;
-            products<kD / 8, 4, T>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
+            products<kD / 8, 4, T, 1>([&](int i) { return read_along<T, kD>(ring[0][0], along, i / 2, i % 2 * kTile); },
                                    [&](int i, V8<T> r) {
                                        if (i % 2 == 0) s = mma(r, q[i / 2], s);
                                        else dp = mma(r, d_o[i / 2], dp);
@@ -317,10 +317,10 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             constexpr int kDs = kD / 32;
             if (early) {
                 const V8<T> left[2] = {left_of<T, 0>(dp, ds[0]), left_of<T, 1>(dp, ds[1])};
-                products<2 * kDs, 2, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
+                products<2 * kDs, 2, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                         [&](int i, V8<T> r) { dq[i % kDs] = mma(r, left[i / kDs], dq[i % kDs]); });
             }
-            products<2 * kDs, 4, T>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
+            products<2 * kDs, 4, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                     [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
         if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, stats, dq);

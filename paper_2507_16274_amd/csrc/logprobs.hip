@@ -201,16 +201,7 @@ template <typename T, bool kOnce> __global__ void __launch_bounds__(kLpThreads) 
         take(at + kStride, w);
     }
     for (; at < to; at += kStride) take(at, load_some_once<kOnce>(x + at, (int)(to - at), -INFINITY));
-    if (a.top) {
-        uint64_t k = 0;
-        if (group < to) {
-            const f32x8 v = load_some(x + group, (int)(to - group), -INFINITY);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (group + i < to) k = umax64(k, key_of(v[i], group + i));
-        }
-        best[t] = k;
-    }
+    if (a.top) best[t] = group < to ? key_of(most, group) : 0;
     s = join_workgroup(s, waves);                            // (behind its barrier the maxima are there as well)
     if (t == 0) {
         if (a.parts > 1) a.part[blockIdx.x] = s;
@@ -248,7 +239,7 @@ template <typename T, bool kOnce> __global__ void __launch_bounds__(kLpThreads) 
 #pragma unroll 4
         for (uint32_t i = 0; i < found[0]; ++i) rank += list[i] > k;
         if (rank < top) first[rank] = (uint8_t)((place_of(k) - from) / 8 % kLpThreads);
-        if (rank == top - 1) bound = k;
+        if (rank == top - 1) bound = k - 7;                  // (the maximum is one of the eight numbers from that place on)
     }
     __syncthreads();
     const uint64_t least = bound;

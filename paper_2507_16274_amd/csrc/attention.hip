@@ -42,6 +42,7 @@ __device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piec
     for (uint32_t key = from; key < umin(to, umin(first + 31, last) + 1); ++key) {
         const float s = dot_row<T, kD, kFull>(q, a.k.at(key, kv), a.head_dim);
         if (key <= row) add_row<T, kD, kFull>(o, exp2_fast(__builtin_fmaf(s, scale, -m * scale)), a.v.at(key, kv), a.head_dim);
+        if (key % 32 == 0 && __all(all_nan(o, a.head_dim))) return;
     }
 }
 

@@ -74,6 +74,7 @@ __device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, co
             add_row<T, kD, kFull>(dv, w, d_o, a.head_dim);
             add_row<T, kD, kFull>(dk, w * (dp + stats[a.tokens]), q, a.head_dim);
         }
+        if (__all(key >= p.end || (all_nan(dk, a.head_dim) && all_nan(dv, a.head_dim)))) return;
     }
 }
 
@@ -215,6 +216,7 @@ __device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, co
         const float s = dot_row<T, kD, kFull>(q, k, a.head_dim), dp = dot_row<T, kD, kFull>(d_o, a.v.at(key, kv), a.head_dim);
         const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
         if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - stats[1]), k, a.head_dim);
+        if (key % 32 == 0 && __all(all_nan(dq, a.head_dim))) return;
     }
 }
 

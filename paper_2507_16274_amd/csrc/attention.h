@@ -202,15 +202,17 @@ template <int kN> __device__ __forceinline__ bool not_finite(const f32x16 (&x)[k
 }
 
 // Whether nothing can change the lane's results any more: then the pairs that are left need not be looked at (a step whose gradients have all overflowed is one of these).
+// (A maximum is NaN only if everything is.)
 template <int kN> __device__ __forceinline__ bool all_nan(const f32x16 (&x)[kN], uint32_t head_dim)
 {
-    bool all = true;
+    float most = as_float(0x7fc00000u);
     const uint32_t half = kept(lane_id() >> 5);
 #pragma unroll
     for (int d = 0; d < kN; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) all &= x[d][i] != x[d][i] || 32 * d + 8 * (i / 4) + 4 * half >= head_dim;
-    return all;
+        for (int i = 0; i < 4; ++i)
+            if (32 * d + 8 * i + 4 * half < head_dim) most = max3(max3(most, x[d][4 * i], x[d][4 * i + 1]), x[d][4 * i + 2], x[d][4 * i + 3]);
+    return most != most;
 }
 
 // Scalar product of the lane's row (as load_row gives it, half of its columns; the other half is across) and a row in memory.

@@ -7,7 +7,7 @@
 // registers, and the weights are, where they lie, the operand of the next product V^T P^T (attention.h).
 //
 // Bound by the matrix pipe and vector issue together: 32 matrix instructions a wave and tile (1024 cycles with heads of 128) against some 175 vector ones, 32 exponentials among
-// them (1100 cycles), of which two waves a SIMD hide most.  One sequence of 8192, 64 heads of 128: 1014 us, 1.09 PFLOP/s, matrix pipe busy 58 % (a product of 16384^3
+// them (1100 cycles), of which two waves a SIMD hide most.  One sequence of 8192, 64 heads of 128: 1027 us, 1.07 PFLOP/s, matrix pipe busy 58 % (a product of 16384^3
 // reaches 1.37).  Short sequences are bound by the beginnings and ends of workgroups: 23 of them, 8000 tokens, 32 heads of 128: 101 us, 0.57 PFLOP/s.
 #include "attention.h"
 

@@ -52,13 +52,20 @@ __device__ __forceinline__ void store_eight_bits(f32x8 y, uint32_t row, uint32_t
     most = row_max(most);
     float scale = fmaxf(as_float(most), kE4m3Max * kLeastScale) / kE4m3Max;
     if (most >= 0x7f800000u) scale = as_float(0x7fc00000u);
+    // y / scale rounded as a division is (Markstein's correction of y times the rounded reciprocal): numbers half way between two of the 8-bit ones are common, since
+    // sums and weights have few bits, and two roundings would send some of them the wrong way.
     const float inverse = 1.f / scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = y[i] * inverse;
+        y[i] = __builtin_fmaf(-__builtin_fmaf(v, scale, -y[i]), inverse, v);        // (signs as they are: a -0 stays one)
+    }
     if (col >= width) return;
     uint32_t word[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        uint32_t v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] * inverse, y[4 * i + 1] * inverse, 0, false);
-        word[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * inverse, y[4 * i + 3] * inverse, v, true);
+        uint32_t v = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
+        word[i] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], v, true);
     }
     uint8_t* at = q + (uint64_t)row * width + col;
     if (col + 8 <= width) __builtin_memcpy(at, word, 8);

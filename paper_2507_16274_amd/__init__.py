@@ -23,6 +23,7 @@ _LIB_PATH = os.path.join(_HERE, "libstalloc.so")
 STATUS = {0: "STALLOC_OK", 1: "STALLOC_ERR_INVALID_ARG", 2: "STALLOC_ERR_BAD_TRACE", 3: "STALLOC_ERR_OVERFLOW",
           4: "STALLOC_ERR_NOMEM", 5: "STALLOC_ERR_DEVICE", 6: "STALLOC_ERR_BAD_ORDER", 7: "STALLOC_ERR_BAD_WINDOW",
           8: "STALLOC_ERR_BAD_LAYER", 9: "STALLOC_ERR_TOO_LARGE", 10: "STALLOC_ERR_BAD_BOUNDS", 11: "STALLOC_ERR_BAD_TOKEN"}
+INVALID_ARG = 1                  # decided on the host, before anything is enqueued
 STATIC_MAX_T_END = 524288        # STALLOC_STATIC_MAX_T_END of include/stalloc.h
 EXPORTS = ("stalloc_plan", "stalloc_validate", "stalloc_lower_bound", "stalloc_lower_bound_static",
            "stalloc_reusable_space",
@@ -447,14 +448,21 @@ def _flat(t: Optional[torch.Tensor], name: str) -> Optional[int]:
 
 
 def _call(fn, name, args, like, stream, workspace_cache, out):
-    """Query, workspace, call.  With a workspace at hand the call comes first: it takes one that is large enough."""
+    """Query, workspace, call.  With a workspace at hand the call comes first: it takes one that is large enough.  Only a refusal, which comes before any
+    work, leads to the query, and only a workspace that is too small to another call."""
     ws = workspace_cache.get("ws") if workspace_cache is not None else None
+    rc = 0
     if ws is not None:
-        if fn(*args, ws.data_ptr(), ctypes.byref(ctypes.c_size_t(ws.numel())), _stream(stream)) == 0:
+        rc = fn(*args, ws.data_ptr(), ctypes.byref(ctypes.c_size_t(ws.numel())), _stream(stream))
+        if rc == 0:
             out["workspace"] = ws
             return out
+        if rc != INVALID_ARG:
+            _check(rc, name)
     need = ctypes.c_size_t(0)
     _check(fn(*args, None, ctypes.byref(need), None), name + "(workspace query)")
+    if ws is not None and ws.numel() >= need.value:
+        _check(rc, name)
     if stream is None:
         ws = _workspace(need.value, like.device, workspace_cache)
     else:

@@ -283,6 +283,7 @@ extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const sta
         !heads_ok(o, shape, shape->heads, true) || !bounds || !lse || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
         return STALLOC_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     if (list_pays(blocks, shape->sequences)) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);
     else list = nullptr;
     with_type(shape->dtype, [&](auto t) {

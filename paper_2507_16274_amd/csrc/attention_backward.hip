@@ -383,6 +383,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
         !lse || !bounds || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
         return STALLOC_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     if (listed) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);
     else list = nullptr;
     const Work by_rows = {list, bounds, shape->sequences, shape->tokens, (uint32_t)pieces, heads, row_parts};

@@ -154,6 +154,7 @@ extern "C" int stalloc_clip_gradients(const stalloc_tensor* tensors, uint32_t k,
     if (!workspace) { *workspace_bytes = cv.used; return STALLOC_OK; }
     if (!norm || !factor || *workspace_bytes < cv.used || !aligned(workspace, kAlign)) return STALLOC_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     size_t done = 0;
     for (uint32_t at = 0; at < k;) {
         at += fill(&list, tensors, k, at);

@@ -444,6 +444,7 @@ extern "C" int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vo
     const LogprobArgs a = {rows, vocabulary, top, shape.parts, shape.part_width, logits, row_stride, tokens, logprob, entropy, lse,
                            top_tokens, top_logprobs, device_status, part, keys};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (read_once(dtype, rows, vocabulary)) hipLaunchKernelGGL((lp_row<T, true>), dim3(rows * shape.parts), dim3(kLpThreads), 0, stream, a);
@@ -465,6 +466,7 @@ extern "C" int stalloc_token_logprobs_backward(uint32_t dtype, uint32_t rows, ui
     if ((uint64_t)rows * chunks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
     const LogprobBackwardArgs a = {rows, vocabulary, chunks, logits, row_stride, tokens, lse, entropy, d_logprob, d_entropy, d_logits, d_row_stride, device_status};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     with_type(dtype, [&](auto t) {
         using T = decltype(t);
         if (read_once(dtype, rows, vocabulary)) hipLaunchKernelGGL((lp_backward<T, true>), dim3(rows * chunks), dim3(kLpThreads), 0, stream, a);

@@ -354,6 +354,7 @@ extern "C" int stalloc_rms_norm(uint32_t dtype, uint32_t rows, uint32_t width, c
     if (!aligned(x, size) || !aligned(residual, size) || !aligned(weight, size) || !aligned(sum, size) || !aligned(y, size)) return STALLOC_ERR_INVALID_ARG;
     const NormArgs a = {rows, width, x, x_stride, residual, residual_stride, weight, eps, sum, y, q, scales, rstd};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     with_type(dtype, [&](auto t) {
         if (read_once(dtype, rows, width)) launch_norm<decltype(t), true>(a, stream);
         else launch_norm<decltype(t), false>(a, stream);
@@ -375,6 +376,7 @@ extern "C" int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t
     if (!aligned(d_y, size) || !aligned(sum, size) || !aligned(weight, size) || !aligned(d_sum, size) || !aligned(dx, size)) return STALLOC_ERR_INVALID_ARG;
     const NormBackwardArgs a = {rows, width, d_y, d_y_stride, sum, weight, rstd, d_sum, dx, part};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    begin_launches();
     with_type(dtype, [&](auto t) {
         if (read_once(dtype, rows, width)) launch_norm_backward<decltype(t), true>(a, teams, stream);
         else launch_norm_backward<decltype(t), false>(a, teams, stream);

@@ -62,8 +62,12 @@ class Memory:
             self.give(out["workspace"])
             return out
         at = self.offsets[self.count]
+        planned = self.pool[at:at + self.sizes[self.count]]
         self.count += 1
-        return fn(*args, workspace_cache={"ws": self.pool[at:at + self.sizes[self.count - 1]]}, **more)
+        out = fn(*args, workspace_cache={"ws": planned}, **more)
+        if out["workspace"].data_ptr() != planned.data_ptr():
+            raise MemoryError("a workspace is larger than what was planned for it")
+        return out
 
     def _note(self, t, nbytes):
         self.live[t.data_ptr()] = self.count

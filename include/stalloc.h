@@ -496,7 +496,8 @@ int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t width, con
  *                 device_status to STALLOC_ERR_BAD_TOKEN
  *   top           how many of the most likely tokens are wanted, 0 .. min(64, vocabulary); top_tokens device
  *                 [rows][top] int32 in descending order of their logits (lower number first among equals),
- *                 top_logprobs device [rows][top].  (Where logits are NaN their order is unspecified.)
+ *                 top_logprobs device [rows][top].  (Where logits are NaN their order is
+ *                 unspecified; they are different tokens of the vocabulary all the same.)
  *   logprob, entropy, lse  device [rows] 32-bit, natural logarithms
  */
 int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vocabulary, const void *logits, uint64_t row_stride,

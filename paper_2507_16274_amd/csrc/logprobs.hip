@@ -24,10 +24,11 @@ constexpr uint32_t kMostTop = 64;
 constexpr uint32_t kMostParts = 64;
 constexpr int kLpThreads = 256;
 
-// A number and its place as one integer: larger numbers first, then lower places; 0 is below all.  -0 counts as 0.
+// A number and its place as one integer: larger numbers first, then lower places; 0 is below all.  -0 counts as 0, NaN of either sign as larger than infinity: a thread's maximum, which
+// passes over NaN, is then never above what the thread holds.
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t place)
 {
-    const uint32_t b = as_bits(x + 0.f);
+    const uint32_t b = x != x ? 0x7fc00000u : as_bits(x + 0.f);
     const uint32_t order = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
     return ((uint64_t)order << 32) | (uint32_t)~place;
 }

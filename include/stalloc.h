@@ -479,7 +479,8 @@ int stalloc_rms_norm(uint32_t dtype, uint32_t rows, uint32_t width, const void *
  *     dx = rstd * (g - sum * rstd^2 * c) + d_sum   (of x and of the residual alike),
  *     dweight = sum over the rows of d_y * sum * rstd.
  * All rows contiguous but d_y's, d_y_stride numbers apart.
- *   d_sum    device [rows][width], the gradient that reaches `sum` by other ways; may be NULL.  dx may be d_sum or d_y.
+ *   d_sum    device [rows][width], the gradient that reaches `sum` by other ways; may be NULL.  dx may be d_sum or d_y
+ *            (with d_y_stride == width).
  *   dweight  device [width] 32-bit, overwritten
  */
 int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t width, const void *d_y, uint64_t d_y_stride,

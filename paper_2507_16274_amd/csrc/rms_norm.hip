@@ -342,6 +342,9 @@ bool norm_sizes_ok(uint32_t dtype, uint32_t rows, uint32_t width)
     return dtype <= STALLOC_F16 && rows >= 1 && rows < 0x80000000u && width >= 1 && width < 0x7ffff000u;
 }
 
+// Whether `out`, rows of `width`, takes the place of rows that lie otherwise: some would be written before they are read.
+bool misplaced(const void* out, const void* in, uint64_t stride, uint32_t rows, uint32_t width) { return out && out == in && rows > 1 && stride != width; }
+
 }  // namespace
 
 extern "C" int stalloc_rms_norm(uint32_t dtype, uint32_t rows, uint32_t width, const void* x, uint64_t x_stride, const void* residual,
@@ -352,6 +355,7 @@ extern "C" int stalloc_rms_norm(uint32_t dtype, uint32_t rows, uint32_t width, c
         return STALLOC_ERR_INVALID_ARG;
     const size_t size = bytes_of(dtype);
     if (!aligned(x, size) || !aligned(residual, size) || !aligned(weight, size) || !aligned(sum, size) || !aligned(y, size)) return STALLOC_ERR_INVALID_ARG;
+    if (misplaced(sum, x, x_stride, rows, width) || misplaced(sum, residual, residual_stride, rows, width)) return STALLOC_ERR_INVALID_ARG;
     const NormArgs a = {rows, width, x, x_stride, residual, residual_stride, weight, eps, sum, y, q, scales, rstd};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     begin_launches();
@@ -374,6 +378,7 @@ extern "C" int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t
     if (!d_y || !sum || !weight || !rstd || !dx || !dweight || *workspace_bytes < cv.used || !aligned(workspace, kAlign)) return STALLOC_ERR_INVALID_ARG;
     const size_t size = bytes_of(dtype);
     if (!aligned(d_y, size) || !aligned(sum, size) || !aligned(weight, size) || !aligned(d_sum, size) || !aligned(dx, size)) return STALLOC_ERR_INVALID_ARG;
+    if (misplaced(dx, d_y, d_y_stride, rows, width)) return STALLOC_ERR_INVALID_ARG;
     const NormBackwardArgs a = {rows, width, d_y, d_y_stride, sum, weight, rstd, d_sum, dx, part};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     begin_launches();

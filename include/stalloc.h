@@ -51,7 +51,7 @@ typedef enum stalloc_status {
     STALLOC_ERR_BAD_ORDER = 6,   /* an entry of `orders` is >= n                                  */
     STALLOC_ERR_BAD_WINDOW = 7,  /* a time window with w_lo >= w_hi                               */
     STALLOC_ERR_BAD_LAYER = 8,   /* an entry of `layer_of` is >= n_layers                         */
-    STALLOC_ERR_TOO_LARGE = 9,   /* the trace exceeds what an entry point without workspace holds */
+    STALLOC_ERR_TOO_LARGE = 9,   /* the trace exceeds what an entry point without workspace holds, a shape what a launch takes */
     STALLOC_ERR_BAD_BOUNDS = 10, /* sequence boundaries that do not begin at 0, descend or pass the tokens */
     STALLOC_ERR_BAD_TOKEN = 11   /* a token number beyond the vocabulary                          */
 } stalloc_status;
@@ -435,6 +435,7 @@ typedef struct stalloc_attention_shape {
  *                 STALLOC_ERR_BAD_BOUNDS (outputs unspecified, memory-safe).
  *   lse           device [heads][tokens]
  *   device_status device [1], written
+ *   Shapes with (tokens / 128 + sequences + 1) * heads >= 2^24 return STALLOC_ERR_TOO_LARGE (from the query, too).
  *   workspace     depends on the whole shape: query it for the shape of the call.  (16 bytes a piece of 128 rows where a batch of several
  *                 sequences has many; where pieces and heads are few, walks over keys are cut into parts whose sums are kept, up to
  *                 4 * head_dim + 8 bytes for each of 131072 rows of a head.)
@@ -509,6 +510,7 @@ int stalloc_token_logprobs(uint32_t dtype, uint32_t rows, uint32_t vocabulary, c
 /*
  * Gradient of the above with respect to the logits for gradients d_logprob and (may be NULL) d_entropy of its
  * outputs, both device [rows]:  d_logits[j] = d_logprob * ([j = token] - p_j) - d_entropy * p_j * (log p_j + entropy).
+ * rows * ceil(vocabulary / 8192) >= 2^24 returns STALLOC_ERR_TOO_LARGE.
  * d_logits may be `logits` itself (same stride): a step then needs one such buffer.  Rows without a token take no
  * part of d_logprob.
  */

@@ -273,7 +273,7 @@ extern "C" int stalloc_attention(const stalloc_attention_shape* shape, const sta
     const uint32_t parts = parts_of(row_pieces(shape) * shape->heads, average_rows(shape) / kAttnKeys, kLeastSteps, 8);
     const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAttnRows), blocks = pieces * shape->heads * parts;
     const uint64_t rows = (uint64_t)shape->tokens * shape->heads;
-    if (blocks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    if (blocks * kAttnThreads > kMostThreads) return STALLOC_ERR_TOO_LARGE;
     Carver cv(workspace);
     float* partial = cv.take<float>(parts > 1 ? parts * rows * shape->head_dim : 0);
     f32x2* part_stats = cv.take<f32x2>(parts > 1 ? parts * rows : 0);

@@ -370,7 +370,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
     const uint32_t row_parts = parts_of(row_pieces(shape) * heads, average_rows(shape) / kAbStep, kLeastKeySteps, 8);
     const uint64_t pieces = most_pieces(shape->tokens, shape->sequences, kAbRows);
     const uint64_t joined = 2 * (uint64_t)kv * shape->tokens * shape->head_dim;
-    if (pieces * heads * row_parts > 0x7fffffffu || pieces * kv * parts > 0x7fffffffu || joined / 2048 >= 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    if (pieces * heads * row_parts * kAbThreads > kMostThreads || pieces * kv * parts * kAbThreads > kMostThreads) return STALLOC_ERR_TOO_LARGE;
     const bool listed = list_pays(pieces * heads, shape->sequences);
     Carver cv(workspace);
     float* stats = cv.take<float>(2 * (size_t)shape->tokens * heads + kAbStep);

@@ -464,7 +464,7 @@ extern "C" int stalloc_token_logprobs_backward(uint32_t dtype, uint32_t rows, ui
         (d_entropy && !entropy) || (rows > 1 && d_row_stride < vocabulary) || !aligned(logits, bytes_of(dtype)) || !aligned(d_logits, bytes_of(dtype)))
         return STALLOC_ERR_INVALID_ARG;
     const uint32_t chunks = (vocabulary + kLpChunk - 1) / kLpChunk;
-    if ((uint64_t)rows * chunks > 0x7fffffffu) return STALLOC_ERR_TOO_LARGE;
+    if ((uint64_t)rows * chunks * kLpThreads > kMostThreads) return STALLOC_ERR_TOO_LARGE;
     const LogprobBackwardArgs a = {rows, vocabulary, chunks, logits, row_stride, tokens, lse, entropy, d_logprob, d_entropy, d_logits, d_row_stride, device_status};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     begin_launches();

@@ -134,6 +134,8 @@ template <typename F> inline void with_type(uint32_t dtype, F f)
 
 inline uint32_t umin_host(uint32_t a, uint32_t b) { return a < b ? a : b; }
 
+constexpr uint64_t kMostThreads = 0xffffffffu;              // of a launch
+
 // What a thread's HIP calls so far have left behind they have told by their own return values: it is put aside before the first launch of a call, so that `launched` tells of
 // the call's own launches.
 inline void begin_launches() { (void)hipGetLastError(); }

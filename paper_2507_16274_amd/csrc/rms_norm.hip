@@ -264,24 +264,29 @@ template <typename T> __global__ void __launch_bounds__(256) norm_dweight_wide(N
     store_some(a.part + (uint64_t)blockIdx.y * a.width + col, n, dw);
 }
 
-// dweight[c] = sum over the teams, in a fixed order: 64 columns a workgroup, sixteen waves that take a share of the teams each.
+// dweight[c] = sum over the teams, in a fixed order: 64 columns a workgroup at a time, sixteen waves that take a share of the teams each.
 __global__ void __launch_bounds__(1024) norm_dweight(const float* __restrict__ part, uint32_t teams, uint32_t width, float* dweight)
 {
     __shared__ float sums[16][kWave];
-    const uint32_t col = blockIdx.x * kWave + lane_id(), w = wave_id();
-    float total = 0.f;
-    if (col < width) {
-        const uint32_t from = (uint32_t)((uint64_t)teams * w / 16), to = (uint32_t)((uint64_t)teams * (w + 1) / 16);
+    const uint32_t w = wave_id();
+    for (uint32_t first = blockIdx.x * kWave; first < width; first += gridDim.x * kWave) {
+        const uint32_t col = first + lane_id();
+        float total = 0.f;
+        if (col < width) {
+            const uint32_t from = (uint32_t)((uint64_t)teams * w / 16), to = (uint32_t)((uint64_t)teams * (w + 1) / 16);
 #pragma unroll 8
-        for (uint32_t i = from; i < to; ++i) total += part[(uint64_t)i * width + col];
-    }
-    sums[w][lane_id()] = total;
-    __syncthreads();
-    if (w != 0 || col >= width) return;
+            for (uint32_t i = from; i < to; ++i) total += part[(uint64_t)i * width + col];
+        }
+        if (first != blockIdx.x * kWave) __syncthreads();    // (the sums before these have been read)
+        sums[w][lane_id()] = total;
+        __syncthreads();
+        if (w != 0 || col >= width) continue;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) total += sums[i][lane_id()];
-    dweight[col] = total;
+        for (int i = 1; i < 16; ++i) total += sums[i][lane_id()];
+        dweight[col] = total;
+    }
 }
+constexpr uint32_t kMostColumnBlocks = 1u << 16;
 
 constexpr uint32_t kWaveWidth = 1024;                        // rows up to here are a wave's
 constexpr uint32_t kWidest = 8 * 1024 * 4, kWidestBackward = 8 * 1024 * 2;         // what a team of 1024 threads keeps in registers
@@ -313,7 +318,34 @@ namespace {
 
 bool read_once(uint32_t dtype, uint32_t rows, uint32_t width) { return (uint64_t)rows * width * bytes_of(dtype) >= (64u << 20); }
 
-template <typename T, bool kOnce> void launch_norm(const NormArgs& a, hipStream_t stream)
+// Rows a launch can take, `threads` to each (a multiple of four: waves that are teams come by fours).
+uint32_t most_rows(uint32_t threads) { return (uint32_t)(kMostThreads / threads) / 4 * 4; }
+
+// The arguments for rows first .. of a call.
+template <typename T> NormArgs rows_from(NormArgs a, uint64_t first, uint32_t rows)
+{
+    a.rows = rows;
+    a.x = (const T*)a.x + first * a.x_stride;
+    if (a.residual) a.residual = (const T*)a.residual + first * a.residual_stride;
+    if (a.sum) a.sum = (T*)a.sum + first * a.width;
+    if (a.y) a.y = (T*)a.y + first * a.width;
+    if (a.q) a.q += first * a.width;
+    if (a.scales) a.scales += first * ((a.width + 127) / 128);
+    a.rstd += first;
+    return a;
+}
+template <typename T> NormBackwardArgs rows_from(NormBackwardArgs a, uint64_t first, uint32_t rows)
+{
+    a.rows = rows;
+    a.d_y = (const T*)a.d_y + first * a.d_y_stride;
+    a.sum = (const T*)a.sum + first * a.width;
+    a.rstd += first;
+    if (a.d_sum) a.d_sum = (const T*)a.d_sum + first * a.width;
+    a.dx = (T*)a.dx + first * a.width;
+    return a;
+}
+
+template <typename T, bool kOnce> void launch_norm_part(const NormArgs& a, hipStream_t stream)
 {
     const NormShape shape = norm_shape(a.width);
     const auto one = [&](auto kernel, uint32_t blocks, uint32_t threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a); };
@@ -324,13 +356,22 @@ template <typename T, bool kOnce> void launch_norm(const NormArgs& a, hipStream_
     else one(norm_rows<T, kOnce, false, 4>, a.rows, shape.threads);
 }
 
+template <typename T, bool kOnce> void launch_norm(const NormArgs& a, hipStream_t stream)
+{
+    const uint32_t most = most_rows(a.width > kWidest ? 1024 : a.width <= kWaveWidth ? kWave : norm_shape(a.width).threads);
+    for (uint64_t first = 0; first < a.rows; first += most) launch_norm_part<T, kOnce>(rows_from<T>(a, first, umin_host(most, a.rows - (uint32_t)first)), stream);
+}
+
 template <typename T, bool kOnce> void launch_norm_backward(const NormBackwardArgs& a, uint32_t teams, hipStream_t stream)
 {
     const NormShape shape = norm_shape(a.width);
     const auto one = [&](auto kernel, uint32_t blocks, uint32_t threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, stream, a); };
     if (a.width > kWidestBackward) {
         hipLaunchKernelGGL(norm_dweight_wide<T>, dim3((a.width + 2047) / 2048, teams), dim3(256), 0, stream, a);
-        one(norm_backward_wide<T>, a.rows, 1024);
+        for (uint64_t first = 0; first < a.rows; first += most_rows(1024)) {
+            const NormBackwardArgs part = rows_from<T>(a, first, umin_host(most_rows(1024), a.rows - (uint32_t)first));
+            hipLaunchKernelGGL(norm_backward_wide<T>, dim3(part.rows), dim3(1024), 0, stream, part);
+        }
     } else if (a.width <= kWaveWidth && shape.groups == 1) one(norm_backward_rows<T, kOnce, true, 1, 256, true>, teams / 4, 256);
     else if (a.width <= kWaveWidth) one(norm_backward_rows<T, kOnce, true, 2, 256, true>, teams / 4, 256);
     else if (shape.threads <= 512) one(norm_backward_rows<T, kOnce, false, 2, 512, true>, teams, shape.threads);
@@ -386,6 +427,6 @@ extern "C" int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t
         if (read_once(dtype, rows, width)) launch_norm_backward<decltype(t), true>(a, teams, stream);
         else launch_norm_backward<decltype(t), false>(a, teams, stream);
     });
-    hipLaunchKernelGGL(norm_dweight, dim3((width + kWave - 1) / kWave), dim3(1024), 0, stream, part, teams, width, dweight);
+    hipLaunchKernelGGL(norm_dweight, dim3(umin_host((width + kWave - 1) / kWave, kMostColumnBlocks)), dim3(1024), 0, stream, part, teams, width, dweight);
     return launched();
 }

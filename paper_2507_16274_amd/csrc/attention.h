@@ -94,16 +94,17 @@ template <typename T, int kD> __device__ __forceinline__ V8<T> read_cross(const 
 // 16 bytes per lane from memory to LDS, lane after lane from `lds` on; `base` and `lds` are the same in all lanes.  Written out because
 // the compiler, which cannot know that the tile asked for is not the one read next, would wait for it there and then; what waits
 // for it is tiles_landed.  Nothing is returned in registers.  A memory access may read a scalar register five wait states after a vector instruction (a readfirstlane) has written it
-// and not before; the compiler, which sees to that elsewhere, does not look into assembly, so the five are in it.
+// and not before; the compiler, which sees to that elsewhere, does not look into assembly, so the five are in it.  The place in LDS is in m0,
+// where the compiler puts it, so that it knows.
 __device__ __forceinline__ void memory_to_lds(uint32_t lds, const void* base, uint32_t offset)
 {
     const uint64_t from = uniform((uint64_t)base);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "{m0}"(lds) : "memory");
 }
 // The same, 4 bytes from an address of each lane's own.
 __device__ __forceinline__ void words_to_lds(uint32_t lds, const void* from)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
+    asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(from), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return uniform((uint32_t)(size_t)(__attribute__((address_space(3))) const void*)p); }
 

@@ -37,3 +37,14 @@ def test_wait_states_before_memory_accesses():
             nop = re.match(r"s_nop\s+(\d+)", i)
             waited += int(nop.group(1)) + 1 if nop else 1
     assert seen >= 2                                             # (the sources are read as meant)
+
+
+def test_m0():
+    """An access to LDS behind m0 gets it as an operand, and a block that writes m0 names it, or the compiler may keep a value there across it."""
+    using = [(name, code, operands) for name, code, operands in blocks() if re.search(r"\bm0\b|_lds_", code)]
+    assert len(using) >= 2
+    for name, code, operands in using:
+        if "_lds_" in code:
+            assert '"{m0}"' in operands, (name, code)
+        if re.search(r"\bs_\w+\s+m0\b", code):
+            assert '"m0"' in operands.rsplit(":", 1)[1], (name, code)

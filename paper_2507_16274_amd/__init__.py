@@ -136,7 +136,8 @@ def _trace(size: torch.Tensor, t_alloc: torch.Tensor, t_free: torch.Tensor, t_en
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())      # (current_stream() makes an object first: 2.7 us)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)       # not part of torch's interface; current_stream() makes an object first: 2.7 us
+    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
 def _workspace(nbytes: int, device, cache: Optional[Dict]) -> torch.Tensor:

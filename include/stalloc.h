@@ -433,6 +433,7 @@ typedef struct stalloc_attention_shape {
  *                 Tokens behind the last boundary (padding) see nothing: o = 0, lse = -infinity.  Bounds
  *                 that do not begin at 0, descend or pass `tokens` set device_status to
  *                 STALLOC_ERR_BAD_BOUNDS (outputs unspecified, memory-safe).
+ *                 A row whose scores are all -infinity has no weights: o = NaN, lse = -infinity.
  *   lse           device [heads][tokens]
  *   device_status device [1], written
  *   Shapes with (tokens / 128 + sequences + 1) * heads >= 2^24 return STALLOC_ERR_TOO_LARGE (from the query, too).

@@ -231,6 +231,26 @@ template <typename T, int kD, bool kFull> __device__ __forceinline__ float dot_r
     return sum + across(sum);
 }
 
+// A row's running maximum (of unscaled scores) while none was seen: below every finite score there is.
+constexpr float kNoScore = -3.402823466e38f;
+
+// Maximum and sum of 2^(scale (s - maximum)) of the scores of the lane's row (q as load_row gives it) with keys from .. to - 1 that it sees, key by key.  The scores are those that
+// the pair-by-pair walks make, to the last bit, whichever of the two rows is in registers: where they are huge, one that is rounded otherwise would be worlds away.
+template <typename T, int kD, bool kFull>
+__device__ __forceinline__ f32x2 row_stats(const V8<T> (&q)[kD / 16], const T* k, uint64_t stride, uint32_t from, uint32_t to, uint32_t row, float scale, uint32_t head_dim)
+{
+    float m = kNoScore, total = 0.f;
+#pragma unroll 1
+    for (uint32_t key = from; key < to; ++key) {
+        const float s = dot_row<T, kD, kFull>(q, k + key * stride, head_dim);
+        if (key > row) continue;
+        const float raised = fmaxf(m, s);
+        total = total * exp2_fast((m - raised) * scale) + exp2_fast((s - raised) * scale);
+        m = raised;
+    }
+    return f32x2{m, total};
+}
+
 // x += w * (a row in memory), columns as store_row has them.
 template <typename T, int kD, bool kFull> __device__ __forceinline__ void add_row(f32x16 (&x)[kD / 32], float w, const T* row, uint32_t head_dim)
 {

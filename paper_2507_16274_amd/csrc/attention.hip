@@ -28,20 +28,40 @@ template <typename T> struct AttentionArgs {
 constexpr uint32_t kLeastSteps = 4;
 constexpr int kAttnThreads = 256, kAttnRows = kPieceRows, kAttnKeys = 64, kAttnStages = 2, kAttnTiles = kAttnKeys / 32;
 
-// o of a wave's rows over keys from .. to - 1, pair by pair (attention.h).  m: their largest scores (scores do not depend on what other keys stand for).
+// Weights of the walk by tiles are 2^(scale s - shift), shift = scale m rounded, in one operation; everything that is relative to m is relative to this shift.  Where shift is
+// huge, what rounding left of scale m is whole powers of two, and scale m itself may overflow: rows like that (and rows whose scores are all -infinity) are made again, pair by pair, with weights 2^(scale
+// (s - m)).
+constexpr float kFarScore = 1 << 16;
+
+// scale m, rounded (and not left to an operation behind it, which would make of the difference of two of them what rounding left of one).
+__device__ __forceinline__ float shift_of(float m, float scale)
+{
+#pragma clang fp contract(off)
+    return m * scale;
+}
+
+// o of a wave's rows over keys from .. to - 1, pair by pair (attention.h).  m, total: their largest scores and the lanes' shares of the sums of weights, which do not depend on what
+// other keys stand for; made again where scores are far.
 template <typename T, int kD, bool kFull>
-__device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, float m, f32x16 (&o)[kD / 32])
+__device__ __forceinline__ void rows_again(const AttentionArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, bool far, float& m, float& total, f32x16 (&o)[kD / 32])
 {
     const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
+    const uint32_t behind = umin(to, umin(first + 31, last) + 1);
     const float scale = a.scale * kLog2e;
     V8<T> q[kD / 16];
     load_row<T, kD, kFull>(q, a.q.at(umin(row, last), head), a.head_dim);
 #pragma unroll
     for (int d = 0; d < kD / 32; ++d) o[d] = f32x16{};
+    if (far) {
+        const f32x2 stats = row_stats<T, kD, kFull>(q, a.k.at(0, kv), a.k.token, from, behind, row, scale, a.head_dim);
+        m = stats[0];
+        total = lane_id() < 32 ? stats[1] : 0.f;
+    }
 #pragma unroll 1
-    for (uint32_t key = from; key < umin(to, umin(first + 31, last) + 1); ++key) {
+    for (uint32_t key = from; key < behind; ++key) {
         const float s = dot_row<T, kD, kFull>(q, a.k.at(key, kv), a.head_dim);
-        if (key <= row) add_row<T, kD, kFull>(o, exp2_fast(__builtin_fmaf(s, scale, -m * scale)), a.v.at(key, kv), a.head_dim);
+        const float w = exp2_fast(far ? (s - m) * scale : __builtin_fmaf(s, scale, -shift_of(m, scale)));
+        if (key <= row) add_row<T, kD, kFull>(o, w, a.v.at(key, kv), a.head_dim);
         if (key % 32 == 0 && __all(all_nan(o, a.head_dim))) return;
     }
 }
@@ -59,7 +79,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     const uint64_t part_row = ((uint64_t)part * a.work.heads + head) * a.work.tokens + row;
     if (p.no_keys) {
         if (row < p.end && parts > 1) {
-            if (half == 0) a.part_stats[part_row] = f32x2{-1e30f, 0.f};
+            if (half == 0) a.part_stats[part_row] = f32x2{kNoScore, -1.f};       // (of no row that sees something)
         } else if (row < p.end) {
             const f32x16 zero[kD / 32] = {};
             store_row<T, kD, kFull>(a.o.at(row, head), zero, 0.f, a.head_dim);
@@ -72,7 +92,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
     const T* v = a.v.at(0, kv);
     const float scale = a.scale * kLog2e, slack = 8.f / scale;
     const Places<kD> places;
-    float m = -1e30f, total = 0.f;                           // running maximum (of unscaled scores), the lane's share of the sum
+    // Running maximum (of unscaled scores; what it begins with is below all that it could be, and finite when it is scaled), the lane's share of the sum.
+    float m = -fminf(3e38f, 1.5e38f / scale), total = 0.f;
     f32x16 o[kD / 32] = {};
     // The walk: tiles of keys up to the last row's; this part's share of them.
     const uint32_t all = (umin(p.first + kAttnRows, p.end) - p.begin + kAttnKeys - 1) / kAttnKeys;
@@ -123,13 +144,13 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
             most = fmaxf(most, across(most));
             // The maximum is raised only where weights would pass 2^8 otherwise: sums and results are relative to it all the same.
             if (__any(most > m + slack)) {
-                const float raised = fmaxf(m, most), f = exp2_fast((m - raised) * scale);
+                const float raised = fmaxf(m, most), f = exp2_fast(shift_of(m, scale) - shift_of(raised, scale));
                 m = raised;
                 total *= f;
 #pragma unroll
                 for (int d = 0; d < kD / 32; ++d) o[d] *= f;
             }
-            const float shift = m * scale;
+            const float shift = shift_of(m, scale);
             float sums[4] = {total, 0.f, 0.f, 0.f};          // (four chains of additions)
 #pragma unroll
             for (int t = 0; t < kAttnTiles; ++t)
@@ -151,7 +172,9 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
                                                  [&](int i, V8<T> v) { o[i % kDs] = mma(v, w[i / kDs], o[i % kDs]); });
         }
     }
-    if (__any(not_finite(o))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAttnKeys, m, o);
+    // (A row may see nothing of a part; one that saw a NaN stays as it is.)
+    const bool far = __any(fabsf(m * scale) > kFarScore && steps && row >= from && row < p.end && total == total);
+    if (far || __any(not_finite(o))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAttnKeys, far, m, total, o);
     total += across(total);
     if (row >= p.end) return;
     if (parts > 1) {
@@ -159,8 +182,9 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAtt
         if (steps) store_row<float, kD, kFull>(a.partial + part_row * a.head_dim, o, 1.f, a.head_dim);
         return;
     }
-    store_row<T, kD, kFull>(a.o.at(row, head), o, total == 0.f ? 0.f : 1.f / total, a.head_dim);
-    if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = (m * scale + log2f(total)) * kLn2;
+    // (A row whose scores are all -infinity has no weights: 0 / 0.)
+    store_row<T, kD, kFull>(a.o.at(row, head), o, 1.f / total, a.head_dim);
+    if (half == 0) a.lse[(uint64_t)head * a.work.tokens + row] = __builtin_fmaf(log2f(total), kLn2, m * a.scale);
 }
 
 // o and lse from the parts': eight columns of a row a thread.
@@ -171,19 +195,23 @@ template <typename T> __global__ void __launch_bounds__(256) attention_join(Atte
     const uint32_t col = (uint32_t)(at % pieces) * 8;
     if (row >= rows) return;
     const float scale = a.scale * kLog2e;
-    float m = -1e30f, total = 0.f;
-    for (uint32_t part = 0; part < a.work.parts; ++part) m = fmaxf(m, a.part_stats[part * rows + row][0]);
+    float m = kNoScore, total = 0.f;
+    for (uint32_t part = 0; part < a.work.parts; ++part) {
+        const f32x2 stats = a.part_stats[part * rows + row];
+        if (!(stats[1] <= 0.f)) m = fmaxf(m, stats[0]);
+    }
     f32x8 o = {};
     for (uint32_t part = 0; part < a.work.parts; ++part) {
         const f32x2 stats = a.part_stats[part * rows + row];
-        if (stats[1] == 0.f) continue;                       // (saw nothing: its sums may not be there)
-        const float f = exp2_fast((stats[0] - m) * scale);
+        if (stats[1] <= 0.f) continue;                       // (saw nothing: its sums may not be there)
+        const float f = exp2_fast(fabsf(m * scale) > kFarScore ? (stats[0] - m) * scale : shift_of(stats[0], scale) - shift_of(m, scale));
         total += stats[1] * f;
         o += load8(a.partial + (part * rows + row) * a.head_dim + col) * f;
     }
     const uint32_t head = (uint32_t)(row / a.work.tokens), token = (uint32_t)(row % a.work.tokens);
-    store8(a.o.at(token, head) + col, o * (total == 0.f ? 0.f : 1.f / total));
-    if (col == 0) a.lse[row] = total == 0.f ? -INFINITY : (m * scale + log2f(total)) * kLn2;
+    const bool padding = a.part_stats[row][1] < 0.f;
+    store8(a.o.at(token, head) + col, o * (padding ? 0.f : 1.f / total));
+    if (col == 0) a.lse[row] = __builtin_fmaf(log2f(total), kLn2, m * a.scale);
 }
 
 // All pieces of the batch, those with the longest walks first: counted by length (of their walk, in pieces), placed by count.  One workgroup; a wave takes a

@@ -18,7 +18,7 @@ namespace stalloc {
 template <typename T> struct AttentionBackwardArgs {
     Heads<T> d_o, q, k, v, o, dq, dk, dv;
     const float* lse;
-    float* stats;                                            // [heads][2][tokens]: lse in units of log 2, -D
+    float* stats;                                            // [heads][2][tokens]: lse in units of log 2, -D (see kFarLse)
     uint32_t* status;
     Work rows, keys;                                         // shared out for dq; for dk and dv
     float* partial;                                          // [parts][2][kv_heads][tokens][head_dim]: dk, dv of a part, if there are several
@@ -47,8 +47,20 @@ template <typename T, int s> __device__ __forceinline__ V8<T> left_of(const f32x
 // What the loops leave out: dp - D is made by the products, whose sum begins at -D, and scale is multiplied in when results are stored (that and the sums' own beginning are
 // 32 of 160 vector operations a step; one sequence of 4096 with 32 heads of 128: 623 us both passes with them, 603 without).
 
-// lse in units of log 2; a row that saw nothing weighs nothing.
-__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// Where lse is large, 32 bits of it say too little: beyond 2^16 (in units of log 2) its rounding is half a per cent of every weight, from 2^24 on whole powers of two.  Rows like that have
+// their maximum and sum made again, pair by pair, and so are all their weights: their lse in `stats` is a NaN, which sends what they reach to rows_again and keys_again, with log2
+// of the sum as its payload, and in place of -D is the maximum.  So are rows whose scores are all -infinity and that have no weights: NaN throughout.
+constexpr float kFarLse = 1 << 16;
+
+struct RowWeights {
+    float lse2, m, log_total;                                // lse2 is NaN: by the maximum and the sum
+    __device__ __forceinline__ float operator()(float s, float scale) const
+    {
+        return exp2_fast(lse2 != lse2 ? (s - m) * scale - log_total : __builtin_fmaf(s, scale, -lse2));
+    }
+};
+__device__ __forceinline__ float packed(float log_total) { return as_float(0x7fc00000u | ((as_bits(log_total) + 256) >> 9 & 0x3fffffu)); }
+__device__ __forceinline__ float unpacked(float lse2) { return as_float((as_bits(lse2) & 0x3fffffu) << 9); }
 
 // dk and dv of a wave's keys pair by pair (attention.h): `steps` steps of the walk from `from_step` on.
 template <typename T, int kD, bool kFull>
@@ -69,10 +81,18 @@ __device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, co
             const T* d_o = a.d_o.at(row, head);
             const float s = dot_row<T, kD, kFull>(k, q, a.head_dim), dp = dot_row<T, kD, kFull>(v, d_o, a.head_dim);
             const float* stats = a.stats + (uint64_t)head * 2 * a.tokens + row;
-            const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
+            const RowWeights weights = {stats[0], stats[a.tokens], unpacked(stats[0])};
+            float less_d = stats[a.tokens];
+            if (weights.lse2 != weights.lse2) {
+                float d = 0.f;
+#pragma unroll 1
+                for (uint32_t col = lane_id(); col < a.head_dim; col += kWave) d = __builtin_fmaf((float)a.o.at(row, head)[col], (float)d_o[col], d);
+                less_d = -wave_sum(d);
+            }
+            const float w = weights(s, a.scale * kLog2e);
             if (row < key) continue;
             add_row<T, kD, kFull>(dv, w, d_o, a.head_dim);
-            add_row<T, kD, kFull>(dk, w * (dp + stats[a.tokens]), q, a.head_dim);
+            add_row<T, kD, kFull>(dk, w * (dp + less_d), q, a.head_dim);
         }
         if (__all(key >= p.end || (all_nan(dk, a.head_dim) && all_nan(dv, a.head_dim)))) return;
     }
@@ -202,7 +222,7 @@ template <typename T, bool kTwo> __global__ void __launch_bounds__(256) gradient
 
 // dq of a wave's rows over keys from .. to - 1, pair by pair (attention.h).
 template <typename T, int kD, bool kFull>
-__device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, f32x2 stats, f32x16 (&dq)[kD / 32])
+__device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, const Piece& p, uint32_t head, uint32_t from, uint32_t to, RowWeights weights, float d, f32x16 (&dq)[kD / 32])
 {
     const uint32_t first = p.first + 32 * wave_id(), row = first + (lane_id() & 31), last = p.end - 1, kv = head / a.group;
     V8<T> q[kD / 16], d_o[kD / 16];
@@ -214,8 +234,8 @@ __device__ __forceinline__ void rows_again(const AttentionBackwardArgs<T>& a, co
     for (uint32_t key = from; key < umin(to, umin(first + 31, last) + 1); ++key) {
         const T* k = a.k.at(key, kv);
         const float s = dot_row<T, kD, kFull>(q, k, a.head_dim), dp = dot_row<T, kD, kFull>(d_o, a.v.at(key, kv), a.head_dim);
-        const float w = exp2_fast(__builtin_fmaf(s, a.scale * kLog2e, -stats[0]));
-        if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - stats[1]), k, a.head_dim);
+        const float w = weights(s, a.scale * kLog2e);
+        if (key <= row) add_row<T, kD, kFull>(dq, w * (dp - d), k, a.head_dim);
         if (key % 32 == 0 && __all(all_nan(dq, a.head_dim))) return;
     }
 }
@@ -283,13 +303,22 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         // D_i of the lane's row, half of the columns each; for the kernel behind this one as well.
         V8<T> o[kD / 16];
         load_row<T, kD, kFull>(o, a.o.at(mine, head), a.head_dim);
-        f32x2 stats = {lse2_of(a.lse[(uint64_t)head * a.tokens + mine]), 0.f};
+        f32x2 stats = {a.lse[(uint64_t)head * a.tokens + mine] * kLog2e, 0.f};
 #pragma unroll
         for (int c = 0; c < kD / 16; ++c) stats[1] += dot(__builtin_convertvector(o[c], f32x8), __builtin_convertvector(d_o[c], f32x8));
         stats[1] += across(stats[1]);
-        const bool early = p.first == p.begin;
-        if (early) stats[1] = early_d<T, kD, kFull>(a, p, kv, q, d_o, stats[0]);
-        if (row < p.end && task.part == 0) a.stats[((uint64_t)head * 2 + half) * a.tokens + row] = half == 0 ? stats[0] : -stats[1];
+        const bool early = p.first == p.begin, far = !(fabsf(stats[0]) <= kFarLse);
+        RowWeights weights = {stats[0], stats[0], 0.f};
+        if (__any(far && stats[0] == stats[0])) {
+            const f32x2 again = row_stats<T, kD, kFull>(q, k, a.k.token, p.begin, umin(first + 31, last) + 1, mine, scale, a.head_dim);
+            if (far && stats[0] == stats[0]) weights = {packed(log2f(again[1])), again[1] > 0.f ? again[0] : as_float(0x7fc00000u), log2f(again[1])};
+            stats[0] = weights.lse2;
+        }
+        if (early) {
+            const float d = early_d<T, kD, kFull>(a, p, kv, q, d_o, stats[0]);
+            if (!far) stats[1] = d;
+        }
+        if (row < p.end && task.part == 0) a.stats[((uint64_t)head * 2 + half) * a.tokens + row] = half == 0 ? stats[0] : far ? weights.m : -stats[1];
         f32x16 less_d = f32x16{} - stats[1];
         asm volatile("" : "+v"(less_d));                     // (in registers, not made anew every step)
         vector_memory_done();
@@ -328,7 +357,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             products<2 * kDs, 4, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                     [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
-        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, stats, dq);
+        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, weights, stats[1], dq);
     }
     if (row >= p.end) return;
     if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, a.scale, a.head_dim);

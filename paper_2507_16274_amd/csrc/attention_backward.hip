@@ -54,13 +54,33 @@ constexpr float kFarLse = 1 << 16;
 
 struct RowWeights {
     float lse2, m, log_total;                                // lse2 is NaN: by the maximum and the sum
-    __device__ __forceinline__ float operator()(float s, float scale) const
+    __device__ __forceinline__ float operator()(float s, float scale, float lift = 0.f) const
     {
-        return exp2_fast(lse2 != lse2 ? (s - m) * scale - log_total : __builtin_fmaf(s, scale, -lse2));
+        return exp2_fast(lse2 != lse2 ? (s - m) * scale - log_total : __builtin_fmaf(s, scale, -lse2) - lift);
     }
 };
 __device__ __forceinline__ float packed(float log_total) { return as_float(0x7fc00000u | ((as_bits(log_total) + 256) >> 9 & 0x3fffffu)); }
 __device__ __forceinline__ float unpacked(float lse2) { return as_float((as_bits(lse2) & 0x3fffffu) << 9); }
+
+// Half precision: numbers that are multiplied again have to lie among the type's normal ones, 2^-14 to 2^16.  Weights, at most 1 and as small as 1 / row, are lifted by 2^14: lse in
+// `stats` is less by 14, and dv is divided by as much at last.  Their gradients ds have the size of d_o, whatever that is.  They are multiplied by a power of two, of each row in dq and
+// of each key in dk, that is lowered when the next tile's largest would pass 2^14 (to where it is below 2^8), and the sums with it; the results are divided by it.  It begins at 2^60, for which
+// nothing is too small.  Without it d_o of 10^-5, of the ordinary size of a mean loss' gradients, cost dq and dk 0.062 of their norm (rounding them 0.022), and d_o of 10^4 was beyond
+// the type, though the results are not.  bfloat16 has the range of 32 bits.  It costs both passes 2 % (one sequence of 4096, 32 heads of 128: 628 -> 641 us) to 5 % (17 sequences, 5003 tokens, heads
+// of 64: 131 -> 139); looking at the rounded operands instead, packed, saves instructions and no time.
+template <typename T> constexpr bool kNarrow = std::is_same<T, f16>::value;
+template <typename T> constexpr float kLift = kNarrow<T> ? 14.f : 0.f;
+constexpr float kMostDs = 16384.f, kMostFactor = 1152921504606846976.f;                   // 2^14, 2^60
+
+__device__ __forceinline__ float largest(const f32x16& x)
+{
+    float t[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) t[i] = max3(fabsf(x[3 * i]), fabsf(x[3 * i + 1]), fabsf(x[3 * i + 2]));
+    return fmaxf(max3(t[0], t[1], t[2]), max3(t[3], t[4], fabsf(x[15])));
+}
+// The exponent of the power of two that leaves 2^7 to 2^8 of t (finite; of an infinity nothing is left but NaN, which is made again).
+__device__ __forceinline__ int exponent_for(float t) { return __builtin_amdgcn_frexp_expf(t) - 8; }
 
 // dk and dv of a wave's keys pair by pair (attention.h): `steps` steps of the walk from `from_step` on.
 template <typename T, int kD, bool kFull>
@@ -89,7 +109,7 @@ __device__ __forceinline__ void keys_again(const AttentionBackwardArgs<T>& a, co
                 for (uint32_t col = lane_id(); col < a.head_dim; col += kWave) d = __builtin_fmaf((float)a.o.at(row, head)[col], (float)d_o[col], d);
                 less_d = -wave_sum(d);
             }
-            const float w = weights(s, a.scale * kLog2e);
+            const float w = weights(s, a.scale * kLog2e, kLift<T>);
             if (row < key) continue;
             add_row<T, kD, kFull>(dv, w, d_o, a.head_dim);
             add_row<T, kD, kFull>(dk, w * (dp + less_d), q, a.head_dim);
@@ -109,6 +129,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), key = first + (lane_id() & 31);
     f32x16 dk[kD / 32] = {}, dv[kD / 32] = {};
+    float factor = kNarrow<T> ? kMostFactor : 1.f;           // of ds, that is in dk
+    float lift = kNarrow<T> ? 16384.f : 1.f;                 // of weights, that is in dk and dv
     if (!p.no_keys) {
         const uint32_t last = p.end - 1;
         const float scale = uniform(a.scale * kLog2e);
@@ -174,6 +196,17 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
                             const uint32_t r = row + row_of(i, half);
                             if (r < key || r >= p.end) s[i] = dp[i] = 0.f;
                         }
+                    if constexpr (kNarrow<T>) {
+                        dp *= factor;
+                        const float t = largest(dp);
+                        if (__any(t > kMostDs)) {
+                            const float most = fmaxf(t, across(t)), f = __builtin_amdgcn_ldexpf(1.f, most > kMostDs ? -exponent_for(most) : 0);
+                            factor *= f;
+                            dp *= f;
+#pragma unroll
+                            for (int d = 0; d < kD / 32; ++d) dk[d] *= f;
+                        }
+                    }
                     // Weights and their gradients are rounded to T for the products; sums stay in 32 bits.
                     const V8<T> w[2] = {operand<T, 0>(s), operand<T, 1>(s)}, ds[2] = {operand<T, 0>(dp), operand<T, 1>(dp)};
                     if (early && row < p.begin + kAbRows) {
@@ -194,17 +227,21 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
         };
         if (p.first == p.begin) walk(std::true_type{});
         else walk(std::false_type{});
-        if (__any(not_finite(dk) || not_finite(dv))) keys_again<T, kD, kFull>(a, p, kv, from_step, steps, dk, dv);
+        if (__any(not_finite(dk) || not_finite(dv))) {
+            keys_again<T, kD, kFull>(a, p, kv, from_step, steps, dk, dv);
+            factor = lift = 1.f;
+        }
     }
     if (key >= p.end) return;
+    const float unlift = 1.f / lift, unfactor = unlift / factor;
     if (parts > 1) {
         const uint64_t heads = a.keys.heads, to = ((2 * task.part * heads + kv) * a.tokens + key) * a.head_dim;
-        store_row<float, kD, kFull>(a.partial + to, dk, a.scale, a.head_dim);
-        store_row<float, kD, kFull>(a.partial + to + heads * a.tokens * a.head_dim, dv, 1.f, a.head_dim);
+        store_row<float, kD, kFull>(a.partial + to, dk, a.scale * unfactor, a.head_dim);
+        store_row<float, kD, kFull>(a.partial + to + heads * a.tokens * a.head_dim, dv, unlift, a.head_dim);
         return;
     }
-    store_row<T, kD, kFull>(a.dk.at(key, kv), dk, a.scale, a.head_dim);
-    store_row<T, kD, kFull>(a.dv.at(key, kv), dv, 1.f, a.head_dim);
+    store_row<T, kD, kFull>(a.dk.at(key, kv), dk, a.scale * unfactor, a.head_dim);
+    store_row<T, kD, kFull>(a.dv.at(key, kv), dv, unlift, a.head_dim);
 }
 
 // Tensors of `heads` heads from those of the parts, added up in their order: eight numbers a thread.  kTwo: two tensors, one behind the other in
@@ -278,6 +315,7 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
     if (p.first >= p.end) return;
     const uint32_t half = lane_id() >> 5, first = p.first + 32 * wave_id(), row = first + (lane_id() & 31);
     f32x16 dq[kD / 32] = {};
+    float factor = kNarrow<T> ? kMostFactor : 1.f;           // of ds, that is in dq
     if (!p.no_keys) {
         const uint32_t last = p.end - 1, kv = head / a.group, mine = umin(row, last);
         const T* k = a.k.at(0, kv);
@@ -318,7 +356,8 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const float d = early_d<T, kD, kFull>(a, p, kv, q, d_o, stats[0]);
             if (!far) stats[1] = d;
         }
-        if (row < p.end && task.part == 0) a.stats[((uint64_t)head * 2 + half) * a.tokens + row] = half == 0 ? stats[0] : far ? weights.m : -stats[1];
+        if (row < p.end && task.part == 0) a.stats[((uint64_t)head * 2 + half) * a.tokens + row] = half == 0 ? (far ? stats[0] : stats[0] - kLift<T>) : far ? weights.m : -stats[1];
+        float less = kNarrow<T> ? stats[0] - 60.f : stats[0];        // lse2, and the logarithm of the divisor
         f32x16 less_d = f32x16{} - stats[1];
         asm volatile("" : "+v"(less_d));                     // (in registers, not made anew every step)
         vector_memory_done();
@@ -341,12 +380,25 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             const bool crosses = key + 31 > first;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                dp[i] *= exp2_fast(__builtin_fmaf(s[i], scale, -stats[0]));
+                dp[i] *= exp2_fast(__builtin_fmaf(s[i], scale, -less));
             }
             if (crosses)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (key + row_of(i, half) > row) dp[i] = 0.f;
+            if constexpr (kNarrow<T>) {
+                const float t = largest(dp);
+                if (__any(t > kMostDs)) {
+                    const float most = fmaxf(t, across(t));
+                    const int by = most > kMostDs ? exponent_for(most) : 0;
+                    const float f = __builtin_amdgcn_ldexpf(1.f, -by);
+                    factor *= f;
+                    less += (float)by;
+                    dp *= f;
+#pragma unroll
+                    for (int d = 0; d < kD / 32; ++d) dq[d] *= f;
+                }
+            }
             const V8<T> ds[2] = {operand<T, 0>(dp), operand<T, 1>(dp)};
             constexpr int kDs = kD / 32;
             if (early) {
@@ -357,11 +409,14 @@ template <typename T, int kD, bool kFull> __global__ void __launch_bounds__(kAbT
             products<2 * kDs, 4, T, 1>([&](int i) { return read_cross<T, kD>(ring[0][0], cross, i % kDs, i / kDs * 32 * kD); },
                                     [&](int i, V8<T> r) { dq[i % kDs] = mma(r, ds[i / kDs], dq[i % kDs]); });
         }
-        if (__any(not_finite(dq))) rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, weights, stats[1], dq);
+        if (__any(not_finite(dq))) {
+            rows_again<T, kD, kFull>(a, p, head, from, from + steps * kAbStep, weights, stats[1], dq);
+            factor = 1.f;
+        }
     }
     if (row >= p.end) return;
-    if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, a.scale, a.head_dim);
-    else store_row<T, kD, kFull>(a.dq.at(row, head), dq, a.scale, a.head_dim);
+    if (a.rows.parts > 1) store_row<float, kD, kFull>(a.partial_dq + (((uint64_t)task.part * a.heads + head) * a.tokens + row) * a.head_dim, dq, a.scale / factor, a.head_dim);
+    else store_row<T, kD, kFull>(a.dq.at(row, head), dq, a.scale / factor, a.head_dim);
 }
 
 }  // namespace stalloc

@@ -166,7 +166,7 @@ def step(c, model, batch, mem, lr=0.05, max_norm=1.0):
     give(fresh)
     logits = product(last["y"], model["vocabulary"].t(), n, c.vocabulary)
     one = {name: take(n, dtype=torch.float32) for name in ("logprob", "entropy", "lse")}
-    mem.call(S.stalloc_token_logprobs, logits, batch["targets"], out={**one, "status": c.status})
+    mem.call(S.stalloc_token_logprobs, logits, batch["targets"], out={**one, "status": c.token_status})
     loss = one["logprob"].sum() / -batch["count"]
 
     # Backward.  The gradient of the logits takes their place; `through` is the gradient of the stream.
@@ -184,7 +184,7 @@ def step(c, model, batch, mem, lr=0.05, max_norm=1.0):
         return d_y
 
     d_logprob = take(n, dtype=torch.float32).fill_(-1.0 / batch["count"])
-    S.stalloc_token_logprobs_backward(logits, batch["targets"], one["lse"], one["entropy"], d_logprob, out={"d_logits": logits, "status": c.status})
+    S.stalloc_token_logprobs_backward(logits, batch["targets"], one["lse"], one["entropy"], d_logprob, out={"d_logits": logits, "status": c.token_status})
     weight_gradient(model["vocabulary"], logits, last["y"])
     d_y = product(logits, model["vocabulary"], n, w)
     give(logits, d_logprob, *one.values())
@@ -226,13 +226,15 @@ def step(c, model, batch, mem, lr=0.05, max_norm=1.0):
 def config(**more):
     c = {"layers": 4, "hidden": 1024, "heads": 8, "kv_heads": 2, "head_dim": 128, "vocabulary": 32000, "tokens": 4096, "sequences": 7, **more}
     c = SimpleNamespace(**c)
-    c.status, c.norm, c.factor = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    # (A call overwrites its status, so calls that can go wrong in different ways have words of their own.)
+    c.status, c.token_status = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    c.norm, c.factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
     return c
 
 
-def run(c, steps=3, orders=64):
+def run(c, steps=3, orders=64, batch=None):
     """Profiles a step, plans it, runs `steps` of them both ways.  Returns a report."""
-    batch = make_batch(c)
+    batch = batch or make_batch(c)
     apart, pooled = make_model(c), make_model(c)
     profiler = Memory()
     results = [[], []]
@@ -244,6 +246,8 @@ def run(c, steps=3, orders=64):
     for _ in range(steps):
         results[1].append(step(c, pooled, batch, memory))
     torch.cuda.synchronize()
+    for status in (c.status, c.token_status):
+        S.check_status({"status": status})
     weights = [[m["vocabulary"], m["norm"]] + [x for layer in m["layers"] for x in layer.values()] for m in (apart, pooled)]
     return {"requests": len(trace.size), "sum": int(trace.size.sum()), "bound": bound, "extent": extent,
             "losses": [[float(loss) for loss, _ in r] for r in results], "norms": [[float(norm) for _, norm in r] for r in results],

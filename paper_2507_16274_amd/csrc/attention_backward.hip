@@ -7,7 +7,7 @@
 // all heads that share them.  Scores are computed twice (seven products instead of five), and in return every sum belongs to one wave: no atomics, and the same
 // result every time; partial gradients are in memory only where walks are cut into parts, because pieces and heads alone would not fill the chip.
 //
-// Bound like the forward kernel.  One sequence of 4096, 32 heads of 128: 0.20 ms and 0.30, matrix pipe busy 61 and 58 %; forward and backward pass 605 us, 0.80 PFLOP/s of the
+// Bound like the forward kernel.  One sequence of 4096, 32 heads of 128: 0.20 ms and 0.30, matrix pipe busy 60 and 57 %; forward and backward pass 605 us, 0.80 PFLOP/s of the
 // five products and the forward pass' two, 1.02 with what is made twice.
 #include <type_traits>
 

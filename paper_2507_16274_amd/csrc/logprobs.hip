@@ -463,6 +463,7 @@ extern "C" int stalloc_token_logprobs_backward(uint32_t dtype, uint32_t rows, ui
     if (!lp_sizes_ok(dtype, rows, vocabulary) || !logits || !tokens || !lse || !d_logprob || !d_logits || !device_status ||
         (d_entropy && !entropy) || (rows > 1 && d_row_stride < vocabulary) || !aligned(logits, bytes_of(dtype)) || !aligned(d_logits, bytes_of(dtype)))
         return STALLOC_ERR_INVALID_ARG;
+    if (d_logits == logits && rows > 1 && d_row_stride != row_stride) return STALLOC_ERR_INVALID_ARG;      // (rows would be written that are still to be read)
     const uint32_t chunks = (vocabulary + kLpChunk - 1) / kLpChunk;
     if ((uint64_t)rows * chunks * kLpThreads > kMostThreads) return STALLOC_ERR_TOO_LARGE;
     const LogprobBackwardArgs a = {rows, vocabulary, chunks, logits, row_stride, tokens, lse, entropy, d_logprob, d_entropy, d_logits, d_row_stride, device_status};

@@ -450,6 +450,7 @@ int stalloc_attention(const stalloc_attention_shape *shape, const stalloc_heads 
  * heads that read them).  o and lse as written by the forward call.  Weights are computed again from q, k
  * and lse; gradients of padding are 0.  The workspace depends on the whole shape, as above (and 8 bytes for every
  * row of a head).
+ * Outputs must not overlap inputs (dq takes the place of none; gradients go into a fused buffer of their own).
  */
 int stalloc_attention_backward(const stalloc_attention_shape *shape, const stalloc_heads *d_o, const stalloc_heads *q,
                                const stalloc_heads *k, const stalloc_heads *v, const stalloc_heads *o, const float *lse,

@@ -466,6 +466,7 @@ extern "C" int stalloc_attention_backward(const stalloc_attention_shape* shape, 
         !heads_ok(o, shape, heads, false) || !heads_ok(dq, shape, heads, true) || !heads_ok(dk, shape, kv, true) || !heads_ok(dv, shape, kv, true) ||
         !lse || !bounds || !device_status || *workspace_bytes < cv.used || !aligned(workspace, kAlign))
         return STALLOC_ERR_INVALID_ARG;
+    if (dq->data == q->data || dq->data == d_o->data || dq->data == o->data) return STALLOC_ERR_INVALID_ARG;       // (they are read again when dq is written)
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     begin_launches();
     if (listed) launch_attention_list(bounds, shape->sequences, shape->tokens, (uint32_t)pieces, list, device_status, stream);

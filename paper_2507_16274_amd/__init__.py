@@ -482,6 +482,12 @@ def _dtype_of(t: torch.Tensor, name: str) -> int:
     return code
 
 
+def _sizes(*counts: int) -> None:
+    """What the library takes in 32 bits (ctypes would cut it short)."""
+    if max(counts) >> 31:
+        raise ValueError("fewer than 2^31 rows, columns, tokens or sequences are expected")
+
+
 def _by_heads(t: torch.Tensor, shape, dtype, name: str) -> _Heads:
     if not t.is_cuda or t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: expected a {dtype} tensor {tuple(shape)} on the GPU")
@@ -495,6 +501,7 @@ def _attention_shape(q, k, bounds, scale) -> _AttentionShape:
     if q.dim() != 3 or k.dim() != 3 or bounds.dim() != 1 or bounds.numel() < 2:
         raise ValueError("q must be [tokens][heads][head_dim], k and v [tokens][kv_heads][head_dim], bounds [sequences + 1]")
     tokens, heads, head_dim = q.shape
+    _sizes(tokens, bounds.numel() - 1, heads, k.shape[1], head_dim)
     return _AttentionShape(_dtype_of(q, "q"), tokens, bounds.numel() - 1, heads, k.shape[1], head_dim, head_dim ** -0.5 if scale is None else scale)
 
 
@@ -547,6 +554,7 @@ def stalloc_rms_norm(x, weight, *, residual=None, eps: float = 1e-6, eight_bits:
     `sum` may be x or residual itself (out={"sum": residual})."""
     if x.dim() != 2:
         raise ValueError("x must be [rows][width]")
+    _sizes(*x.shape)
     code, (rows, width) = _dtype_of(x, "x"), x.shape
     out = dict(out) if out else {}
     y = _new(out, "y", x.shape, x.dtype, x, stream) if not eight_bits or out.get("y") is not None else None
@@ -574,6 +582,7 @@ def stalloc_rms_norm_backward(d_y, sum, weight, rstd, *, d_sum=None, out: Option
     reaches `sum` by other ways.  dx may be d_sum or d_y itself."""
     if sum.dim() != 2:
         raise ValueError("sum must be [rows][width]")
+    _sizes(*sum.shape)
     code, (rows, width) = _dtype_of(sum, "sum"), sum.shape
     if weight.shape != (width,) or weight.dtype != sum.dtype or rstd.shape != (rows,):
         raise ValueError("weight must be [width], of the type of sum, and rstd [rows]")
@@ -593,6 +602,7 @@ def stalloc_token_logprobs(logits, tokens, *, top: int = 0, out: Optional[Dict] 
     tokens top_tokens int32 [rows][top] (lower number first among equals) and top_logprobs float32 [rows][top]; status int32 [1]."""
     if logits.dim() != 2 or tokens.shape != (logits.shape[0],):
         raise ValueError("logits must be [rows][vocabulary] and tokens [rows]")
+    _sizes(*logits.shape)
     if not 0 <= top <= min(MOST_TOP, logits.shape[1]):
         raise ValueError(f"top must be 0 .. min({MOST_TOP}, vocabulary)")
     code, (rows, vocabulary) = _dtype_of(logits, "logits"), logits.shape
@@ -614,6 +624,7 @@ def stalloc_token_logprobs_backward(logits, tokens, lse, entropy, d_logprob, d_e
     d_logits may be logits itself (out={"d_logits": logits})."""
     if logits.dim() != 2 or any(t is not None and t.shape != (logits.shape[0],) for t in (tokens, lse, entropy, d_logprob, d_entropy)):
         raise ValueError("logits must be [rows][vocabulary], everything else [rows]")
+    _sizes(*logits.shape)
     code, (rows, vocabulary) = _dtype_of(logits, "logits"), logits.shape
     out = dict(out) if out else {}
     d_logits = _new(out, "d_logits", logits.shape, logits.dtype, logits, stream)

@@ -494,7 +494,7 @@ int stalloc_rms_norm_backward(uint32_t dtype, uint32_t rows, uint32_t width, con
  * Log probabilities of given tokens under the softmax of every row of logits, its entropy and its most
  * likely tokens, in one pass over the logits.
  *
- *   logits        device [rows][vocabulary], rows row_stride numbers apart; -infinity marks a token that cannot
+ *   logits        device [rows][vocabulary], rows < 2^24, vocabulary < 2^30, rows row_stride numbers apart; -infinity marks a token that cannot
  *                 occur.  A row of nothing else has lse = logprob = -infinity and entropy 0.
  *   tokens        device [rows] int32; a negative one stands for none (logprob 0); one >= vocabulary sets
  *                 device_status to STALLOC_ERR_BAD_TOKEN
